@@ -320,6 +320,84 @@ int tt_batch_matmul(const void *a, const void *b, void *c, const tt_gemm_shape *
 int tt_dwconv(const void *x, const void *w, const void *bias, void *y, const tt_conv_shape *shape,
               const tt_schedule *sched, void *stream);
 
+/*
+ * Matrices held in 8 bits.  A matrix [rows, cols] is e4m3 (OCP: largest finite value 448) in rows of
+ * kp = ceil(cols / 128) * 128 bytes, zeros behind cols, and one float32 scale for `block_rows` rows (1: activations, 128: weights;
+ * the last block of rows may be lower) by 128 columns: scale[b][r / block_rows] belongs to columns 128 b .. 128 b + 127, the rows'
+ * scales of one column block next to each other, so that a step along the reduction reads its scales as one run.  Element (r, j)
+ * stands for value[r][j] * scale[j / 128][r / block_rows].  A batch is that many such matrices one behind the other, values and
+ * scales apart.
+ *
+ * tt_quantize_fp8: x [batch, rows, cols] of `dtype` into that form.  For every block a = max(max |x|, 2^-100), scale = a / 448,
+ * value = x * (448 / a), all in float32, rounded to nearest even.  A block that holds an infinity or a NaN has that as its
+ * scale, and everything computed from the block is NaN.
+ */
+#define TT_FP8_BLOCK 128
+typedef struct tt_quant_shape {
+    int32_t batch, rows, cols;
+    int32_t block_rows; /* 1 or 128 */
+    int32_t dtype;      /* tt_dtype of x */
+} tt_quant_shape;
+int tt_quantize_fp8(const void *x, void *q, float *scale, const tt_quant_shape *shape, void *stream);
+
+/*
+ * Products of such matrices: c[b,m,n] = act(bias[n] + sum over column blocks j of a_scale[j][m] * b_scale[j][n / b_rows] *
+ * sum over the block of a[m,.] * b[n,.]).  a has a scale per row, b per `b_rows` rows.  `dtype` is that of c and bias.
+ * The sum over the blocks is float32.  Inside a block: float32 results (TT_F32) are summed in float32, by the bf16 matrix cores,
+ * which every e4m3 value fits exactly.  bf16 results are summed by the 8-bit matrix cores, twice as fast; those add products in
+ * runs of eight and cut each off 13 bits below the largest of its run, so that a result is off by less than 7 * 2^-13 of the sum
+ * of its absolute products (rows of normal values: 2^-16 of the result, where a bf16 result's own rounding is 2^-8).
+ *   tt_dense_fp8         classes TT_DENSE_ADD, TT_DENSE_BIAS_RELU, TT_DENSE_BIAS_GELU; batch 1; bias may be NULL
+ *   tt_batch_matmul_fp8  no bias, no activation; any batch
+ * They stand outside the schedule records: the library chooses the launch from the shape, tt_fp8_plan says which, and how large a
+ * workspace it needs (none: 0).  1 <= k <= 2^22, and rows of outputs by their tile at most 2^31 - 1 workgroups (else
+ * TT_ERR_UNSUPPORTED).
+ */
+typedef struct tt_fp8_shape {
+    int32_t batch, m, n, k;
+    int32_t b_rows; /* rows of b that share a scale: 1 or 128 */
+    int32_t dtype;  /* tt_dtype of c and bias */
+} tt_fp8_shape;
+enum tt_fp8_kernel { TT_FP8_DIRECT = 0, TT_FP8_TILES = 1, TT_FP8_BLOCKS = 2 };
+typedef struct tt_fp8_launch {
+    int32_t kernel; /* tt_fp8_kernel */
+    int32_t tile_m, tile_n, split_k;
+    int32_t grid, block, lds_bytes; /* grid: of one batch entry and one split */
+    int32_t reserved;
+    int64_t workspace_bytes;
+} tt_fp8_launch;
+int tt_fp8_plan(const tt_fp8_shape *shape, tt_fp8_launch *launch);
+int tt_dense_fp8(const void *x, const float *x_scale, const void *w, const float *w_scale, const void *bias, void *y,
+                 const tt_fp8_shape *shape, int cls, void *ws, size_t ws_bytes, void *stream);
+int tt_batch_matmul_fp8(const void *a, const float *a_scale, const void *b, const float *b_scale, void *c,
+                        const tt_fp8_shape *shape, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Group norm + activation over channels-last activations: x, y [n,h,w,c], the channels in `groups` runs of c / groups;
+ * y = act((x - mean) / sqrt(var + eps) * gamma[c] + beta[c]), mean and (biased) variance over the pixels and channels of an
+ * (image, group), in float32 from differences to the mean.  gamma, beta [c] of x's type, or NULL for ones and zeros.
+ * tt_group_norm_act_fp8 writes act's float32 values as a matrix held in 8 bits instead, [n * h * w, c] with a scale per pixel
+ * and 128 channels: the left operand of tt_dense_fp8 for a pointwise convolution or dense layer.
+ * Partial statistics live in the workspace: tt_norm_plan says how large it is (none: 0).  eps >= 0.
+ */
+typedef enum tt_act { TT_ACT_NONE = 0, TT_ACT_RELU = 1, TT_ACT_RELU6 = 2, TT_ACT_GELU = 3, TT_ACT_SILU = 4 } tt_act;
+typedef struct tt_norm_shape {
+    int32_t n, h, w, c, groups; /* groups divides c */
+    int32_t dtype;              /* tt_dtype of x, gamma, beta, y */
+} tt_norm_shape;
+enum tt_norm_kernel { TT_NORM_TWO_PASS = 0, TT_NORM_ONE_PASS = 1 };
+typedef struct tt_norm_launch {
+    int32_t kernel; /* tt_norm_kernel */
+    int32_t chunks; /* partial statistics of an (image, group) */
+    int32_t grid, block;
+    int64_t workspace_bytes;
+} tt_norm_launch;
+int tt_norm_plan(const tt_norm_shape *shape, int fp8, tt_norm_launch *launch);
+int tt_group_norm_act(const void *x, const void *gamma, const void *beta, void *y, const tt_norm_shape *shape, int act,
+                      float eps, void *ws, size_t ws_bytes, void *stream);
+int tt_group_norm_act_fp8(const void *x, const void *gamma, const void *beta, void *q, float *scale,
+                          const tt_norm_shape *shape, int act, float eps, void *ws, size_t ws_bytes, void *stream);
+
 /* One target kernel of a sweep.  bufs: conv {x, w, bias, residual|NULL, y}; dense {x, w, bias, y, NULL};
  * batch matmul {a, b, c, NULL, NULL}; depthwise {x, w, bias, y, NULL}.
  * alt_bufs (host array of n_alt x 5 device pointers, NULL when n_alt = 0): further tensor sets of the same

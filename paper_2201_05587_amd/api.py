@@ -77,6 +77,28 @@ class tt_plan(Structure):
         return self.status == TT_OK and self.variant_id >= 0
 
 
+class tt_quant_shape(Structure):
+    _fields_ = [(n, c_int32) for n in ("batch", "rows", "cols", "block_rows", "dtype")]
+
+
+class tt_fp8_shape(Structure):
+    _fields_ = [(n, c_int32) for n in ("batch", "m", "n", "k", "b_rows", "dtype")]
+
+
+class tt_fp8_launch(Structure):
+    _fields_ = [(n, c_int32) for n in ("kernel", "tile_m", "tile_n", "split_k", "grid", "block", "lds_bytes", "reserved")]
+    _fields_ += [("workspace_bytes", c_int64)]
+
+
+class tt_norm_shape(Structure):
+    _fields_ = [(n, c_int32) for n in ("n", "h", "w", "c", "groups", "dtype")]
+
+
+class tt_norm_launch(Structure):
+    _fields_ = [(n, c_int32) for n in ("kernel", "chunks", "grid", "block")]
+    _fields_ += [("workspace_bytes", c_int64)]
+
+
 class tt_kernel_desc(Structure):
     _fields_ = [("cls", c_int32), ("use_count", c_int32), ("shape", c_void_p), ("bufs", c_void_p * 5),
                 ("ws", c_void_p), ("ws_bytes", c_size_t), ("alt_bufs", POINTER(c_void_p)), ("n_alt", c_int32)]
@@ -99,7 +121,8 @@ class tt_sweep_row(Structure):
 
 EXPORTS = ("tt_version", "tt_status_name", "tt_last_error", "tt_schedule_default", "tt_schedule_apply", "tt_plan_tile",
            "tt_debug_tile_map", "tt_debug_launch", "tt_debug_list", "tt_debug_fast_div", "tt_debug_probe", "tt_conv2d_bias_relu", "tt_conv2d_bias_relu_noalloc", "tt_dense_bias_relu", "tt_batch_matmul", "tt_dwconv",
-           "tt_transfer_sweep", "tt_sweep_plan", "tt_refine_space", "tt_refine", "tt_native_sweep", "tt_time_pair", "tt_run_kernels", "tt_run_kernels_as_recorded", "tt_schedule_space", "tt_sweep_select", "tt_variant_info", "tt_num_variants", "tt_select_donor")
+           "tt_transfer_sweep", "tt_sweep_plan", "tt_refine_space", "tt_refine", "tt_native_sweep", "tt_time_pair", "tt_run_kernels", "tt_run_kernels_as_recorded", "tt_schedule_space", "tt_sweep_select", "tt_variant_info", "tt_num_variants", "tt_select_donor",
+           "tt_quantize_fp8", "tt_fp8_plan", "tt_dense_fp8", "tt_batch_matmul_fp8", "tt_norm_plan", "tt_group_norm_act", "tt_group_norm_act_fp8")
 
 
 def _load():
@@ -151,6 +174,13 @@ def _load():
                                     POINTER(c_double), ctypes.c_int, POINTER(tt_sweep_row)]
     lib.tt_select_donor.argtypes = [POINTER(c_double), ctypes.c_int, POINTER(c_int32), ctypes.c_int, POINTER(c_double),
                                     POINTER(c_int32)]
+    lib.tt_quantize_fp8.argtypes = [c_void_p] * 3 + [POINTER(tt_quant_shape), c_void_p]
+    lib.tt_fp8_plan.argtypes = [POINTER(tt_fp8_shape), POINTER(tt_fp8_launch)]
+    lib.tt_dense_fp8.argtypes = [c_void_p] * 6 + [POINTER(tt_fp8_shape), ctypes.c_int, c_void_p, c_size_t, c_void_p]
+    lib.tt_batch_matmul_fp8.argtypes = [c_void_p] * 5 + [POINTER(tt_fp8_shape), c_void_p, c_size_t, c_void_p]
+    lib.tt_norm_plan.argtypes = [POINTER(tt_norm_shape), ctypes.c_int, POINTER(tt_norm_launch)]
+    lib.tt_group_norm_act.argtypes = [c_void_p] * 4 + [POINTER(tt_norm_shape), ctypes.c_int, c_float, c_void_p, c_size_t, c_void_p]
+    lib.tt_group_norm_act_fp8.argtypes = [c_void_p] * 5 + [POINTER(tt_norm_shape), ctypes.c_int, c_float, c_void_p, c_size_t, c_void_p]
     for name in EXPORTS:
         if name not in ("tt_status_name", "tt_last_error", "tt_debug_fast_div"):
             getattr(lib, name).restype = ctypes.c_int
@@ -295,7 +325,8 @@ def _empty_tensor(x, sizes):
     return _torch().empty(sizes, dtype=x.dtype, device=x.device)
 
 
-_ttcall.bind(tt_conv_shape, tt_gemm_shape, tt_schedule, _refuse_struct, _empty_tensor)
+_ttcall.bind(tt_conv_shape, tt_gemm_shape, tt_schedule, _refuse_struct, _empty_tensor, tt_quant_shape, tt_fp8_shape,
+             tt_norm_shape)
 
 
 def _result(out, where):
@@ -330,6 +361,54 @@ def tt_batch_matmul(a, b, shape, sched=None, ws=None, c=None):
 
 def tt_dwconv(x, w, bias, shape, sched=None, y=None):
     return _result(_ttcall.dwconv(x, w, bias, to_c_shape(shape), sched, y), "tt_dwconv")
+
+
+# ---- matrices held in 8 bits with a scale for each block of 128, group norm -------------------------------------------
+# The forms are tt.h's.  Values are torch.float8_e4m3fn, scales float32; a tensor of another type, size, layout or device than
+# the shape says is TT_ERR_BAD_ARG.  Outputs and workspaces that the caller does not give are allocated.
+TT_FP8_BLOCK = 128
+TT_FP8_DIRECT = 0
+TT_NORM_TWO_PASS = 0
+TT_ACT_NONE, TT_ACT_RELU, TT_ACT_RELU6, TT_ACT_GELU, TT_ACT_SILU = range(5)
+
+
+def tt_quantize_fp8(x, shape, q=None, scale=None):
+    """(values [batch, rows, kp], scales [batch, kp / 128, row blocks]) of x; `shape`: a tt_quant_shape."""
+    return _result(_ttcall.quantize_fp8(x, shape, q, scale), "tt_quantize_fp8")
+
+
+def tt_fp8_plan(shape) -> tt_fp8_launch:
+    """What a product of this tt_fp8_shape runs on, and the workspace it needs."""
+    out = tt_fp8_launch()
+    _check(lib.tt_fp8_plan(byref(shape), byref(out)), "tt_fp8_plan")
+    return out
+
+
+def tt_dense_fp8(x, x_scale, w, w_scale, bias, shape, cls, ws=None, y=None):
+    """y [m, n] of `shape`'s dtype; cls: TT_DENSE_ADD, TT_DENSE_BIAS_RELU or TT_DENSE_BIAS_GELU; bias may be None."""
+    return _result(_ttcall.dense_fp8(x, x_scale, w, w_scale, bias, shape, cls, ws, y), "tt_dense_fp8")
+
+
+def tt_batch_matmul_fp8(a, a_scale, b, b_scale, shape, ws=None, c=None):
+    """c [batch, m, n] = a b^T."""
+    return _result(_ttcall.matmul_fp8(a, a_scale, b, b_scale, shape, ws, c), "tt_batch_matmul_fp8")
+
+
+def tt_norm_plan(shape, fp8=False) -> tt_norm_launch:
+    """What a group norm of this tt_norm_shape runs on, and the workspace it needs."""
+    out = tt_norm_launch()
+    _check(lib.tt_norm_plan(byref(shape), int(fp8), byref(out)), "tt_norm_plan")
+    return out
+
+
+def tt_group_norm_act(x, gamma, beta, shape, act=TT_ACT_NONE, eps=1e-5, ws=None, y=None):
+    """y [n, h, w, c]; gamma and beta may be None."""
+    return _result(_ttcall.group_norm(x, gamma, beta, shape, act, eps, ws, y), "tt_group_norm_act")
+
+
+def tt_group_norm_act_fp8(x, gamma, beta, shape, act=TT_ACT_NONE, eps=1e-5, ws=None, q=None, scale=None):
+    """The same as 8-bit blocks: (values [n * h * w, cp], scales [cp / 128, n * h * w])."""
+    return _result(_ttcall.group_norm_fp8(x, gamma, beta, shape, act, eps, ws, q, scale), "tt_group_norm_act_fp8")
 
 
 def tt_debug_tile_map(plan):

@@ -44,7 +44,6 @@ extern "C" const char *tt_last_error(void) { return tt::g_last_error; }
 
 namespace {
 
-inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline int conv_out(int in, int f, int stride, int pad) { return (in + 2 * pad - f) / stride + 1; }
 
 // Estimated time (us) of a launch in tiles of tm x tn: a CU takes in 80 GB/s of operand rows and multiplies at 1/256 of

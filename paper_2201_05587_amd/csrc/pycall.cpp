@@ -214,13 +214,190 @@ PyObject *py_dwconv(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// bind(conv shape type, gemm shape type, schedule type, refuse_struct, empty_tensor): once, by the binding
+// ---- matrices held in 8 bits, group norm ----------------------------------------------------------------
+// Unlike the records' operators these know the type and size of every argument, so a tensor is taken only if it is of that
+// type, as large as the shape says, dense, and on the current device.  (What is no plain tensor is the caller's own memory.)
+
+PyObject *quant_shape_type, *fp8_shape_type, *norm_shape_type;
+
+class Checked {
+public:
+    void *address(PyObject *o, at::ScalarType type, int64_t numel)
+    {
+        if (!THPVariable_CheckExact(o)) return address_of(o);
+        const at::Tensor &t = THPVariable_Unpack(o);
+        good_ = good_ && t.scalar_type() == type && t.numel() == numel && t.is_contiguous() && on_device(t);
+        return good_ ? t.data_ptr() : nullptr;
+    }
+    // A workspace is memory of any type; `bytes`: how many there are.
+    void *workspace(PyObject *o, size_t *bytes)
+    {
+        *bytes = o == Py_None ? 0 : bytes_of(o);
+        if (!THPVariable_CheckExact(o)) return address_of(o);
+        const at::Tensor &t = THPVariable_Unpack(o);
+        good_ = good_ && t.is_contiguous() && on_device(t);
+        return good_ ? t.data_ptr() : nullptr;
+    }
+    bool good() const { return good_; }
+
+private:
+    static bool on_device(const at::Tensor &t) { return t.is_cuda() && t.device().index() == c10::hip::current_device(); }
+    bool good_ = true;
+};
+
+at::ScalarType type_of(int32_t dtype) { return dtype == TT_F32 ? at::kFloat : at::kBFloat16; }
+int64_t blocks_of(int64_t n) { return (n + TT_FP8_BLOCK - 1) / TT_FP8_BLOCK; }
+
+// A new tensor on the current device, or the caller's.
+PyObject *output_object(PyObject *given, at::IntArrayRef sizes, at::ScalarType type)
+{
+    if (given != Py_None) return Py_NewRef(given);
+    return THPVariable_Wrap(at::empty(sizes, at::TensorOptions().dtype(type).device(at::kCUDA, c10::hip::current_device())));
+}
+class Workspace {
+public:
+    Workspace(Checked &check, PyObject *given, int64_t needed)
+    {
+        at_ = check.workspace(given, &bytes_);
+        if (given != Py_None || needed == 0 || !check.good()) return;
+        own_ = at::empty({needed}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, c10::hip::current_device()));
+        at_ = own_.data_ptr(), bytes_ = (size_t)needed;
+    }
+    void *at_;
+    size_t bytes_;
+
+private:
+    at::Tensor own_;
+};
+template <class F> int launched(const Checked &check, F &&launch)
+{
+    if (!check.good()) return TT_ERR_BAD_ARG;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS rc = launch();
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+
+// quantize_fp8(x, shape, q, scale)
+PyObject *py_quantize_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 4, "quantize_fp8 takes four arguments");
+    const tt_quant_shape s = struct_of<tt_quant_shape>(a[1], quant_shape_type);
+    if (const int rc = check_quant_shape(s); rc != TT_OK) return PyLong_FromLong(rc);
+    Checked check;
+    const int64_t kb = blocks_of(s.cols), rb = (s.rows + s.block_rows - 1) / s.block_rows;
+    const void *const x = check.address(a[0], type_of(s.dtype), (int64_t)s.batch * s.rows * s.cols);
+    if (!check.good()) return PyLong_FromLong(TT_ERR_BAD_ARG);
+    Owned q(output_object(a[2], {s.batch, s.rows, kb * TT_FP8_BLOCK}, at::kFloat8_e4m3fn));
+    Owned scale(output_object(a[3], {s.batch, kb, rb}, at::kFloat));
+    void *const qp = check.address(q.get(), at::kFloat8_e4m3fn, (int64_t)s.batch * s.rows * kb * TT_FP8_BLOCK);
+    void *const sp = check.address(scale.get(), at::kFloat, s.batch * kb * rb);
+    void *const stream = current_stream();
+    const int rc = launched(check, [&] { return tt_quantize_fp8(x, qp, static_cast<float *>(sp), &s, stream); });
+    return rc == TT_OK ? PyTuple_Pack(2, q.get(), scale.get()) : PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// cls < 0: tt_batch_matmul_fp8
+PyObject *product_fp8(PyObject *ap, PyObject *as, PyObject *bp, PyObject *bs, PyObject *bias, PyObject *shape, int cls, PyObject *ws, PyObject *out)
+{
+    const tt_fp8_shape s = struct_of<tt_fp8_shape>(shape, fp8_shape_type);
+    tt_fp8_launch l;
+    if (cls >= 0 && (!is_dense_class(cls) || s.batch != 1)) return PyLong_FromLong(TT_ERR_BAD_ARG);
+    if (const int rc = tt_fp8_plan(&s, &l); rc != TT_OK) return PyLong_FromLong(rc);
+    Checked check;
+    const int64_t kb = blocks_of(s.k);
+    const void *const a = check.address(ap, at::kFloat8_e4m3fn, (int64_t)s.batch * s.m * kb * TT_FP8_BLOCK);
+    const void *const b = check.address(bp, at::kFloat8_e4m3fn, (int64_t)s.batch * s.n * kb * TT_FP8_BLOCK);
+    const auto *const a_scale = static_cast<const float *>(check.address(as, at::kFloat, s.batch * kb * s.m));
+    const auto *const b_scale = static_cast<const float *>(check.address(bs, at::kFloat, s.batch * kb * ((s.n + s.b_rows - 1) / s.b_rows)));
+    const void *const bi = check.address(bias, type_of(s.dtype), s.n);
+    if (!check.good()) return PyLong_FromLong(TT_ERR_BAD_ARG);
+    const int64_t sizes[3] = {s.batch, s.m, s.n};
+    Owned y(output_object(out, at::IntArrayRef(sizes + (cls >= 0), cls >= 0 ? 2 : 3), type_of(s.dtype)));
+    void *const c = check.address(y.get(), type_of(s.dtype), (int64_t)s.batch * s.m * s.n);
+    const Workspace w(check, ws, l.workspace_bytes);
+    void *const stream = current_stream();
+    const int rc = launched(check, [&] {
+        return cls >= 0 ? tt_dense_fp8(a, a_scale, b, b_scale, bi, c, &s, cls, w.at_, w.bytes_, stream)
+                        : tt_batch_matmul_fp8(a, a_scale, b, b_scale, c, &s, w.at_, w.bytes_, stream);
+    });
+    return rc == TT_OK ? Py_NewRef(y.get()) : PyLong_FromLong(rc);
+}
+// dense_fp8(x, x_scale, w, w_scale, bias, shape, cls, ws, y)
+PyObject *py_dense_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 9, "dense_fp8 takes nine arguments");
+    const int cls = class_of(a[6]);
+    return product_fp8(a[0], a[1], a[2], a[3], a[4], a[5], cls < 0 ? TT_NUM_CLASSES : cls, a[7], a[8]);
+    END_HANDLE_TH_ERRORS
+}
+// matmul_fp8(a, a_scale, b, b_scale, shape, ws, c)
+PyObject *py_matmul_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 7, "matmul_fp8 takes seven arguments");
+    return product_fp8(a[0], a[1], a[2], a[3], Py_None, a[4], -1, a[5], a[6]);
+    END_HANDLE_TH_ERRORS
+}
+
+// `scale` null: tt_group_norm_act
+PyObject *group_norm(PyObject *x, PyObject *gamma, PyObject *beta, PyObject *shape, PyObject *act_of, PyObject *eps_of, PyObject *ws, PyObject *out, PyObject *scale)
+{
+    const tt_norm_shape s = struct_of<tt_norm_shape>(shape, norm_shape_type);
+    const int act = class_of(act_of);
+    const double eps = PyFloat_AsDouble(eps_of);
+    if (eps == -1.0 && PyErr_Occurred()) throw python_error();
+    tt_norm_launch l;
+    if (const int rc = tt_norm_plan(&s, scale != nullptr, &l); rc != TT_OK) return PyLong_FromLong(rc);
+    Checked check;
+    const int64_t rows = (int64_t)s.n * s.h * s.w, kb = blocks_of(s.c);
+    const at::ScalarType type = type_of(s.dtype);
+    const void *const xp = check.address(x, type, rows * s.c);
+    const void *const gp = check.address(gamma, type, s.c), *const bp = check.address(beta, type, s.c);
+    if (!check.good()) return PyLong_FromLong(TT_ERR_BAD_ARG);
+    const Workspace w(check, ws, l.workspace_bytes);
+    void *const stream = current_stream();
+    if (!scale) {
+        Owned y(output_object(out, {s.n, s.h, s.w, s.c}, type));
+        void *const yp = check.address(y.get(), type, rows * s.c);
+        const int rc = launched(check, [&] { return tt_group_norm_act(xp, gp, bp, yp, &s, act, (float)eps, w.at_, w.bytes_, stream); });
+        return rc == TT_OK ? Py_NewRef(y.get()) : PyLong_FromLong(rc);
+    }
+    Owned q(output_object(out, {rows, kb * TT_FP8_BLOCK}, at::kFloat8_e4m3fn)), sc(output_object(scale, {kb, rows}, at::kFloat));
+    void *const qp = check.address(q.get(), at::kFloat8_e4m3fn, rows * kb * TT_FP8_BLOCK);
+    auto *const sp = static_cast<float *>(check.address(sc.get(), at::kFloat, kb * rows));
+    const int rc = launched(check, [&] { return tt_group_norm_act_fp8(xp, gp, bp, qp, sp, &s, act, (float)eps, w.at_, w.bytes_, stream); });
+    return rc == TT_OK ? PyTuple_Pack(2, q.get(), sc.get()) : PyLong_FromLong(rc);
+}
+// group_norm(x, gamma, beta, shape, act, eps, ws, y)
+PyObject *py_group_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 8, "group_norm takes eight arguments");
+    return group_norm(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], nullptr);
+    END_HANDLE_TH_ERRORS
+}
+// group_norm_fp8(x, gamma, beta, shape, act, eps, ws, q, scale)
+PyObject *py_group_norm_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    TORCH_CHECK_TYPE(n == 9, "group_norm_fp8 takes nine arguments");
+    return group_norm(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8]);
+    END_HANDLE_TH_ERRORS
+}
+
+// bind(conv shape type, gemm shape type, schedule type, refuse_struct, empty_tensor, quant shape type, fp8 shape type, norm shape
+// type): once, by the binding
 PyObject *py_bind(PyObject *, PyObject *args)
 {
-    PyObject *o[5];
-    if (!PyArg_ParseTuple(args, "OOOOO", &o[0], &o[1], &o[2], &o[3], &o[4])) return nullptr;
-    PyObject **const slots[5] = {&conv_shape_type, &gemm_shape_type, &schedule_type, &refuse_struct, &empty_tensor};
-    for (int i = 0; i < 5; ++i) {
+    PyObject *o[8];
+    if (!PyArg_ParseTuple(args, "OOOOOOOO", &o[0], &o[1], &o[2], &o[3], &o[4], &o[5], &o[6], &o[7])) return nullptr;
+    PyObject **const slots[8] = {&conv_shape_type, &gemm_shape_type, &schedule_type, &refuse_struct, &empty_tensor,
+                                 &quant_shape_type, &fp8_shape_type, &norm_shape_type};
+    for (int i = 0; i < 8; ++i) {
         PyObject *const before = *slots[i];
         *slots[i] = Py_NewRef(o[i]);
         Py_XDECREF(before);
@@ -242,6 +419,11 @@ PyMethodDef methods[] = {
     {"dense", (PyCFunction)(void (*)())py_dense, METH_FASTCALL, nullptr},
     {"matmul", (PyCFunction)(void (*)())py_matmul, METH_FASTCALL, nullptr},
     {"dwconv", (PyCFunction)(void (*)())py_dwconv, METH_FASTCALL, nullptr},
+    {"quantize_fp8", (PyCFunction)(void (*)())py_quantize_fp8, METH_FASTCALL, nullptr},
+    {"dense_fp8", (PyCFunction)(void (*)())py_dense_fp8, METH_FASTCALL, nullptr},
+    {"matmul_fp8", (PyCFunction)(void (*)())py_matmul_fp8, METH_FASTCALL, nullptr},
+    {"group_norm", (PyCFunction)(void (*)())py_group_norm, METH_FASTCALL, nullptr},
+    {"group_norm_fp8", (PyCFunction)(void (*)())py_group_norm_fp8, METH_FASTCALL, nullptr},
     {"stream", py_stream, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -418,6 +418,12 @@ int launch_tile_map_dump(const TileMap &map, int32_t *out_dev, void *stream);
 // Compute units of the current device (asked once; one device per process).
 int compute_units();
 
+// Longest rows of matrices held in 8 bits: a tile's rows stay within 32-bit byte offsets.
+constexpr int32_t kFp8LargestK = 1 << 22;
+int check_quant_shape(const tt_quant_shape &s); // (fp8_quantize.hip)
+
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
 // Remember the text of a failed HIP call for tt_last_error(); returns TT_ERR_HIP.
 int note_hip_error(int hip_error_code, const char *where);
 
