@@ -1,0 +1,266 @@
+// Products of matrices held in 8 bits in 256 x 256 blocks (bf16 results), for launches with enough outputs to give every CU one.
+//
+// The order of work is that of contract_block.hip.h, whose slices of 64 bf16 elements are as many bytes as a step of 128 here:
+// eight waves in two teams take turns at the matrix cores, a step is four phases of one quadrant (64 rows of A by 32 of B a
+// wave) each, and every phase requests one region of a later step:
+//
+//   phase      0            1            2            3
+//   multiply   A0 . B0      A0 . B1      A1 . B1      A1 . B0
+//   read       A0           B1           A1           B0 of the next step
+//   request    B1 (t + 1)   A1 (t + 1)   A0 (t + 2)   B0 (t + 2), scales (t + 2)          (step t, buffer t mod 2)
+//
+// What is new is the scaling.  A matrix instruction starts from zero, and its four sums a lane go into the accumulators by FMAs
+// two instructions later, in issue slots that the matrix cores leave free (32 cycles an instruction, 16 of FMAs); the last two
+// of a turn are taken in the next reading turn, so that no wave waits for a product's latency.
+// A step's scales, 256 of A and as many of B, come into the LDS with the operands, in a ring of four.
+#pragma once
+
+#include "fp8_product.hip.h"
+
+namespace tt {
+
+// Position of a row's 16-byte pieces in the LDS: piece c of row r lies at c ^ swizzle(r).  A fragment's 16 lanes read one piece of
+// 16 rows, which the swizzle spreads over all banks (256 bytes, two rows).
+//   rows of A: r, r + 1, ... r + 15;   rows of B: 8 (i / 4) + i % 4 (+ 4), i = 0 .. 15, so that the matrix cores leave eight
+//   consecutive columns of the result in a lane.
+__device__ __forceinline__ int a_swizzle(int r) { return (r >> 1) & 7; }
+__device__ __forceinline__ int b_swizzle(int r) { return ((r >> 1) & 1) | ((r >> 2) & 6); }
+
+__device__ __forceinline__ void load4_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint32_t byte_offset, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                 :
+                 : "s"(lds_addr), "v"(byte_offset), "s"(rsrc)
+                 : "memory", "m0");
+}
+
+// Eight consecutive columns of one row of the result.
+template <int DT> __device__ __forceinline__ void store_eight(void *out, int64_t at, const float (&v)[8], int count);
+template <> __device__ __forceinline__ void store_eight<TT_BF16>(void *out, int64_t at, const float (&v)[8], int count)
+{
+    const u32x4 r = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    store_piece<TT_BF16>(out, at, r, count);
+}
+template <> __device__ __forceinline__ void store_eight<TT_F32>(void *out, int64_t at, const float (&v)[8], int count)
+{
+    store_piece<TT_F32>(out, at, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, min(count, 4));
+    if (count > 4)
+        store_piece<TT_F32>(out, at + 4, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])}, count - 4);
+}
+template <int DT> __device__ __forceinline__ void load_eight(float (&v)[8], const void *p, int64_t at, int count)
+{
+#pragma unroll
+    for (int h = 0; h < 8; h += ElemOf<DT>::CH) {
+        const u32x4 r = count > h ? load_piece<DT>(p, at + h, count - h) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < ElemOf<DT>::CH; ++e) v[h + e] = element_of<DT>(r, e);
+    }
+}
+
+struct Fp8Block {
+    static constexpr int BM = 256, BN = 256, THREADS = 512, STEP = 64, NL = 2; // STEP: rows between the NL loads of a thread
+    static constexpr int ROW = kFp8Block, REGION = 128 * ROW, SLICE = 4 * REGION;
+    static constexpr int SCALES = 512 * 4, RING = 4, LDS = 2 * SLICE + RING * SCALES;
+    static constexpr int BAND = 4;
+};
+
+template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kernel(const ProductArgs g, int blocks_m, int blocks_n)
+{
+    using S = Fp8Block;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const uint32_t lds0 = lds_address(smem);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int team = wave >> 2;
+    const int wm = team, wn = wave & 3; // 64-row strip of every region of A, 32-row strip of every region of B
+
+    // block of this workgroup: a contiguous run per XCD, in bands of four block rows (see contract_block)
+    int m0, n0;
+    {
+        const int total = blocks_m * blocks_n, wg = (int)blockIdx.x;
+        const int per = total / kXcds, rem = total % kXcds, x = wg % kXcds;
+        const int L = x * per + min(x, rem) + wg / kXcds;
+        const int band = L / (S::BAND * blocks_n), at = L - band * S::BAND * blocks_n;
+        const int high = min(S::BAND, blocks_m - band * S::BAND);
+        m0 = (band * S::BAND + at % high) * S::BM;
+        n0 = at / high * S::BN;
+    }
+    const int64_t batch = blockIdx.y;
+    const int kb = g.kb;
+    const uint32_t kp = (uint32_t)kb * kFp8Block;
+    const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(g.a + (batch * g.M + m0) * kp, (uint32_t)min(S::BM, g.M - m0) * kp);
+    const __amdgpu_buffer_rsrc_t b_rsrc = make_rsrc(g.b + (batch * g.N + n0) * kp, (uint32_t)min(S::BN, g.N - n0) * kp);
+    // this thread's piece of its first row of a region: rows past the matrix are past the end of the buffer
+    const int first = tid / 8;
+    const uint32_t a_at = first * kp + ((tid % 8) ^ a_swizzle(first)) * 16, b_at = first * kp + ((tid % 8) ^ b_swizzle(first)) * 16;
+    auto request = [&](__amdgpu_buffer_rsrc_t rsrc, uint32_t at, int region, int h, int t, int buffer) {
+        const uint32_t to = lds0 + (uint32_t)(buffer * S::SLICE + region * S::REGION + wave * 64 * 16);
+#pragma unroll
+        for (int i = 0; i < S::NL; ++i) // (at is below 2^30)
+            load16_to_lds(rsrc, at + (t < kb ? (uint32_t)(h * 128 + i * S::STEP) * kp + (uint32_t)t * kFp8Block : kOutOfRange),
+                          to + (uint32_t)(i * S::THREADS * 16));
+    };
+    auto request_a = [&](int h, int t, int buffer) { request(a_rsrc, a_at, h, h, t, buffer); };
+    auto request_b = [&](int h, int t, int buffer) { request(b_rsrc, b_at, 2 + h, h, t, buffer); };
+    // waves 0-3: the scales of the block's rows of A; waves 4-7: of B (one in 128 rows: the same scale for each of them)
+    const float *const scales = team == 0 ? g.a_scale + batch * kb * g.M + m0 : g.b_scale + batch * kb * g.b_scale_row + n0 / B_ROWS;
+    const int64_t scale_row = team == 0 ? g.M : g.b_scale_row;
+    const uint32_t scale_bytes = 4u * (uint32_t)(team == 0 ? min(S::BM, g.M - m0) : min(S::BN / B_ROWS, g.b_scale_row - n0 / B_ROWS));
+    const uint32_t scale_at = 4u * (uint32_t)(team == 0 ? tid : (tid - 256) / B_ROWS);
+    auto request_scales = [&](int t) {
+        const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(scales + min(t, kb - 1) * scale_row, t < kb ? scale_bytes : 0u);
+        load4_to_lds(rsrc, scale_at, lds0 + (uint32_t)(2 * S::SLICE + (t % S::RING) * S::SCALES + wave * 256));
+    };
+
+    f32x4 acc[2][2][4][2]; // [A region][B region][16 rows of A][16 rows of B]
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[h][k][i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const int lane_r = lane % 16, lane_g = lane / 16;
+    const int a_row = wm * 64 + lane_r, b_row = wn * 32 + lane_r / 4 * 8 + lane_r % 4;
+    // (rows 16 further have A's swizzle unchanged, rows 4 further B's)
+    const int a_from = a_row * S::ROW + (lane_g ^ a_swizzle(a_row)) * 16, b_from = b_row * S::ROW + (lane_g ^ b_swizzle(b_row)) * 16;
+    Fragment af[4], bf[2][2];
+    auto read_a = [&](int h, int buffer) {
+        const unsigned char *const from = smem + buffer * S::SLICE + h * S::REGION;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            af[i].lo = *reinterpret_cast<const u32x4 *>(from + i * 16 * S::ROW + a_from);
+            af[i].hi = *reinterpret_cast<const u32x4 *>(from + i * 16 * S::ROW + (a_from ^ 64));
+        }
+    };
+    auto read_b = [&](Fragment (&to)[2], int h, int buffer) {
+        const unsigned char *const from = smem + buffer * S::SLICE + (2 + h) * S::REGION;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            to[j].lo = *reinterpret_cast<const u32x4 *>(from + j * 4 * S::ROW + b_from);
+            to[j].hi = *reinterpret_cast<const u32x4 *>(from + j * 4 * S::ROW + (b_from ^ 64));
+        }
+    };
+    auto swap_teams = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+    };
+    // the scales of quadrant (h, k) of step t
+    float sa[4], sb[B_ROWS == 1 ? 8 : 1];
+    auto read_scales = [&](int h, int k, int t) {
+        const float *const from = reinterpret_cast<const float *>(smem + 2 * S::SLICE + (t % S::RING) * S::SCALES);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sa[i] = from[h * 128 + a_row + i * 16];
+        if constexpr (B_ROWS == 1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sb[e] = from[256 + k * 128 + wn * 32 + lane_g * 8 + e];
+        } else {
+            sb[0] = from[256 + k * 128];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sa[i] *= sb[0];
+        }
+    };
+    f32x4 part[8]; // products of the matrix instructions of a quadrant, 2 i + j
+    auto accumulate = [&](f32x4 (&c)[4][2], int x) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            c[x / 2][x % 2][e] = fmaf(part[x][e], B_ROWS == 1 ? sa[x / 2] * sb[(x % 2 * 4 + e) % (B_ROWS == 1 ? 8 : 1)] : sa[x / 2], c[x / 2][x % 2][e]);
+    };
+    constexpr int LAG = 2; // matrix instructions issued before the first one's products are used
+    auto multiply = [&](f32x4 (&c)[4][2], const Fragment (&b)[2]) {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            part[x] = BlockProduct<TT_BF16>::run(b[x % 2], af[x / 2]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (x >= LAG) accumulate(c, x - LAG);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+    };
+    auto finish = [&](f32x4 (&c)[4][2]) {
+#pragma unroll
+        for (int x = 8 - LAG; x < 8; ++x) accumulate(c, x);
+    };
+
+    // steps 0 and 1, in the order the loop would have requested them: all but the last two regions of step 1
+    request_a(0, 0, 0), request_b(0, 0, 0), request_scales(0), request_b(1, 0, 0), request_a(1, 0, 0);
+    request_a(0, 1, 1), request_b(0, 1, 1), request_scales(1);
+    wait_loads_outstanding<9>(); // A0, B0 and scales of step 0
+    __syncthreads();
+    read_b(bf[0], 0, 0);
+    if (team == 1) swap_teams(); // team 1 runs one turn behind
+
+    // `buffer`: t mod 2, a constant
+    auto step = [&](int t, int buffer, Fragment (&b0)[2], Fragment (&b1)[2]) {
+        // phase 0
+        read_a(0, buffer);
+        request_b(1, t + 1, buffer ^ 1);
+        if (t > 0) finish(acc[1][0]);
+        read_scales(0, 0, t);
+        wait_loads_outstanding<9>(); // B1 of this step has landed (the other team reads it a turn later)
+        swap_teams();
+        multiply(acc[0][0], b0);
+        swap_teams();
+        // phase 1
+        read_b(b1, 1, buffer);
+        request_a(1, t + 1, buffer ^ 1);
+        finish(acc[0][0]);
+        read_scales(0, 1, t);
+        wait_loads_outstanding<9>(); // A1 of this step
+        swap_teams();
+        multiply(acc[0][1], b1);
+        swap_teams();
+        // phase 2
+        read_a(1, buffer);
+        request_a(0, t + 2, buffer);
+        finish(acc[0][1]);
+        read_scales(1, 1, t);
+        wait_loads_outstanding<6>(); // A0, B0 and scales of the next step
+        swap_teams();
+        multiply(acc[1][1], b1);
+        swap_teams();
+        // phase 3
+        read_b(b1, 0, buffer ^ 1);
+        request_b(0, t + 2, buffer);
+        request_scales(t + 2);
+        finish(acc[1][1]);
+        read_scales(1, 0, t);
+        swap_teams();
+        multiply(acc[1][0], b0);
+        swap_teams();
+    };
+    for (int t = 0; t < kb; t += 2) {
+        step(t, 0, bf[0], bf[1]);
+        if (t + 1 < kb) step(t + 1, 1, bf[1], bf[0]);
+    }
+    finish(acc[1][0]);
+    if (team == 0) swap_teams(); // team 1 is one turn behind
+    wait_loads_outstanding<0>(); // the requests past the end: nothing may still write the LDS when the workgroup ends
+
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int n = n0 + k * 128 + wn * 32 + lane_g * 8;
+        float bias[8] = {};
+        if (g.bias && n < g.N) load_eight<TT_BF16>(bias, g.bias, n, g.N - n);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int m = m0 + h * 128 + a_row + i * 16;
+                if (m >= g.M || n >= g.N) continue;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = acc[h][k][i][e / 4][e % 4] + bias[e];
+                apply_act_all<8>(v, g.act);
+                store_eight<TT_BF16>(g.out, (batch * g.M + m) * g.N + n, v, g.N - n);
+            }
+    }
+}
+
+} // namespace tt

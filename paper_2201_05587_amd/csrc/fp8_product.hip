@@ -1,7 +1,7 @@
 // Products of matrices held in 8 bits, entry points and launch rule.
 #include <hip/hip_runtime.h>
 
-#include "fp8_product.hip.h"
+#include "fp8_block.hip.h"
 
 namespace tt {
 namespace {
@@ -12,6 +12,17 @@ int plan_of(const tt_fp8_shape &s, tt_fp8_launch *l)
     if (s.dtype != TT_F32 && s.dtype != TT_BF16) return TT_ERR_BAD_ARG;
     *l = tt_fp8_launch{};
     if (s.k > kFp8LargestK || s.batch > 65535) return TT_ERR_UNSUPPORTED;
+    const int64_t blocks_m = (s.m + 255ll) / 256, blocks_n = (s.n + 255ll) / 256;
+    if (s.dtype == TT_BF16 && blocks_m * blocks_n * s.batch >= compute_units() / 2) {
+        l->kernel = TT_FP8_BLOCKS;
+        l->tile_m = l->tile_n = 256;
+        l->split_k = 1;
+        if (blocks_m * blocks_n > INT32_MAX) return TT_ERR_UNSUPPORTED;
+        l->grid = (int32_t)(blocks_m * blocks_n);
+        l->block = Fp8Block::THREADS;
+        l->lds_bytes = Fp8Block::LDS;
+        return TT_OK;
+    }
     l->kernel = TT_FP8_DIRECT;
     l->tile_m = l->tile_n = 16;
     l->split_k = 1;
@@ -22,8 +33,20 @@ int plan_of(const tt_fp8_shape &s, tt_fp8_launch *l)
     return TT_OK;
 }
 
+template <int B_ROWS> int launch_blocks(const ProductArgs &g, const tt_fp8_launch &l, void *stream)
+{
+    auto kern = product_block_kernel<B_ROWS>;
+    static DynamicLdsLimit limit;
+    if (const int rc = limit.raise_to(reinterpret_cast<const void *>(kern), l.lds_bytes); rc != TT_OK) return rc;
+    hipLaunchKernelGGL(kern, dim3(l.grid, g.batch), dim3(l.block), l.lds_bytes, static_cast<hipStream_t>(stream), g, (g.M + 255) / 256, (g.N + 255) / 256);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? TT_OK : note_hip_error((int)e, "product_block_kernel launch");
+}
+
 template <int DT> int launch(const ProductArgs &g, const tt_fp8_launch &l, void *stream)
 {
+    if constexpr (DT == TT_BF16)
+        if (l.kernel == TT_FP8_BLOCKS) return g.b_rows == 1 ? launch_blocks<1>(g, l, stream) : launch_blocks<kFp8Block>(g, l, stream);
     hipLaunchKernelGGL((product_direct_kernel<DT>), dim3(l.grid, g.batch), dim3(l.block), 0, static_cast<hipStream_t>(stream), g);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? TT_OK : note_hip_error((int)e, "product_direct_kernel launch");

@@ -145,6 +145,51 @@ def test_batch_matmul(batch, m, n, k, b_rows, dtype):
     check_product(batch, m, n, k, b_rows, dtype)
 
 
+def check_large(batch, m, n, k, b_rows, dtype, cls, seed=3):
+    """The same against float64 products on the GPU, for sizes that the loops of the reference are too slow for."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda *shape: torch.randn(shape, generator=gen, device="cuda")  # noqa: E731
+    a, a_s = api.tt_quantize_fp8(normal(batch, m, k) * torch.exp(0.5 * normal(batch, m, 1)), api.tt_quant_shape(batch, m, k, 1, F32))
+    b, b_s = api.tt_quantize_fp8(normal(batch, n, k), api.tt_quant_shape(batch, n, k, b_rows, F32))
+    shape, kb = api.tt_fp8_shape(batch, m, n, k, b_rows, dtype), -(-k // 128)
+    y = torch.full((batch, m, n), float("nan"), dtype=api.torch_dtype(dtype), device="cuda")
+    bias = normal(n).to(y.dtype) if cls is not None else None
+    if cls is None:
+        api.tt_batch_matmul_fp8(a, a_s, b, b_s, shape, c=y)
+    else:
+        api.tt_dense_fp8(a, a_s, b, b_s, bias, shape, cls, y=y)
+    worst = 0.0
+    for i in range(batch):
+        wide = lambda q, s, g: (q.double().view(-1, kb, 128) * s.double().repeat_interleave(g, dim=1)[:, :q.shape[0]].t().unsqueeze(2)).view(-1, kb * 128)  # noqa: E731
+        x, w = wide(a[i], a_s[i], 1), wide(b[i], b_s[i], b_rows)
+        ref, size = x @ w.t(), x.abs() @ w.abs().t()
+        if bias is not None:
+            ref, size = ref + bias.double(), size + bias.double().abs()
+        if cls == api.TT_DENSE_BIAS_RELU:
+            ref = torch.relu(ref)
+        if cls == api.TT_DENSE_BIAS_GELU:
+            ref = torch.nn.functional.gelu(ref)
+        tol = (128 + 2 * kb + 4) * 2.0 ** -23 * size + (7 * 2.0 ** -13 * size if dtype == BF16 else 0)
+        if cls == api.TT_DENSE_BIAS_GELU:
+            tol = 1.13 * tol + 2.0 ** -20 * ref.abs()
+        if dtype == BF16:
+            tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs()
+        err = (y[i].double() - ref).abs()
+        assert bool((err <= tol).all()), (i, int((~(err <= tol)).sum()), torch.nonzero(~(err <= tol))[:4].tolist(), float((err / tol).max()))
+        worst = max(worst, float((err / tol).max()))
+    return worst
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("b_rows", [1, 128])
+@pytest.mark.parametrize("batch,m,n,k", [(1, 2900, 3001, 640), (1, 4100, 2051, 200), (1, 2048, 4096, 128), (1, 4096, 2049, 256), (1, 2500, 3500, 384),
+                                         (1, 3840, 2304, 1000), (1, 1030, 768, 4096), (1, 129, 4097, 8192), (1, 8192, 24, 1024), (40, 300, 520, 333),
+                                         (130, 256, 256, 512), (70, 130, 390, 500), (1, 1500, 1700, 5000)])
+def test_products_of_many_tiles(batch, m, n, k, b_rows, dtype):
+    check_large(batch, m, n, k, b_rows, dtype, None if batch > 1 else (api.TT_DENSE_ADD, api.TT_DENSE_BIAS_RELU, api.TT_DENSE_BIAS_GELU)[(m + n) % 3])
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("m", [1, 40, 300, 1100])
@@ -164,7 +209,7 @@ def test_a_product_spreads_what_is_not_a_number_over_its_row_only(m, dtype):
 def test_products_are_the_same_every_time_on_every_stream_and_in_a_graph():
     """Bit for bit, with the caller's workspaces: two calls at once on two streams, and replays of a captured pass."""
     rng = np.random.default_rng(9)
-    for m, n, k, dtype in ((1, 512, 4096, BF16), (24, 1000, 2048, F32), (300, 640, 1024, BF16), (1030, 768, 512, BF16)):
+    for m, n, k, dtype in ((1, 512, 4096, BF16), (24, 1000, 2048, F32), (300, 640, 1024, BF16), (1030, 768, 512, BF16), (4096, 2048, 384, BF16)):
         _, _, a, a_s = held(rng, 1, m, k, 1)
         _, _, b, b_s = held(rng, 1, n, k, 128)
         x = torch.from_numpy(make(rng, 1, m, k)).cuda()
