@@ -13,14 +13,45 @@ TT_HD int64_t fp8_blocks(int64_t cols) { return (cols + kFp8Block - 1) / kFp8Blo
 // infinity above the finite values and NaN above infinity, where fmaxf would drop a NaN.
 __device__ __forceinline__ uint32_t magnitude_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 constexpr uint32_t kFp8Smallest = (127u - 100u) << 23; // 2^-100: below it 448 / a would leave float32's range
-// scale = a / 448 and the factor of the values, 448 / a, each rounded once (the two divisions are per block of 128 or more).
+// scale = a / 448 and the factor of the values, 448 / a, each rounded once.  All lanes of a block form both, so that two of the
+// compiler's divisions (some 24 instructions) would cost a lane of eight values as much as its values; from an approximate reciprocal
+// and the remainder of the quotient they are nine.  Checked for every mantissa of a: both are the rounded quotients.
 struct Fp8Scale {
     float scale, factor;
 };
 __device__ __forceinline__ Fp8Scale fp8_scale(uint32_t largest)
 {
     const float a = __uint_as_float(max(largest, kFp8Smallest));
-    return {a / 448.0f, 448.0f / a};
+    Fp8Scale s;
+    if (largest < (127u + 100u) << 23) { // a and 1 / a far from where float32 ends
+        constexpr float R = 1.0f / 448.0f;
+        const float q = a * R;
+        s.scale = fmaf(fmaf(-448.0f, q, a), R, q);
+        const float r0 = __builtin_amdgcn_rcpf(a), r = fmaf(fmaf(-a, r0, 1.0f), r0, r0), f = 448.0f * r;
+        s.factor = fmaf(fmaf(-a, f, 448.0f), r, f);
+    } else
+        s.scale = a / 448.0f, s.factor = 448.0f / a;
+    return s;
+}
+// The largest magnitude of values, two at a time: as signed integers the positive ones are in order, as unsigned ones the negative
+// ones above them all.
+struct Largest {
+    int32_t positive = 0;
+    uint32_t negative = 0;
+    __device__ __forceinline__ void add(float a, float b)
+    {
+        positive = max(positive, max(__float_as_int(a), __float_as_int(b)));
+        negative = max(negative, max(__float_as_uint(a), __float_as_uint(b)));
+    }
+    __device__ __forceinline__ uint32_t bits() const { return max((uint32_t)positive, negative & ((uint32_t)((int32_t)negative >> 31) >> 1)); }
+};
+// The largest of 16 neighbouring lanes (lanes 16 i .. 16 i + 15), in each of them: rotations inside the row.
+__device__ __forceinline__ uint32_t largest_of_16_lanes(uint32_t v)
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, false)); // row_ror:8, 4, 2, 1
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, false));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, false));
 }
 // Four values to nearest even.  |x| <= a keeps x * factor within 448 * (1 + 2^-23), which rounds to 448: nothing overflows.
 __device__ __forceinline__ uint32_t pack_fp8x4(float a, float b, float c, float d)
