@@ -358,7 +358,7 @@ typedef struct tt_fp8_shape {
     int32_t b_rows; /* rows of b that share a scale: 1 or 128 */
     int32_t dtype;  /* tt_dtype of c and bias */
 } tt_fp8_shape;
-enum tt_fp8_kernel { TT_FP8_DIRECT = 0, TT_FP8_TILES = 1, TT_FP8_BLOCKS = 2 };
+enum tt_fp8_kernel { TT_FP8_STREAM = 0, TT_FP8_TILES = 1, TT_FP8_BLOCKS = 2 };
 typedef struct tt_fp8_launch {
     int32_t kernel; /* tt_fp8_kernel */
     int32_t tile_m, tile_n, split_k;

@@ -367,7 +367,7 @@ def tt_dwconv(x, w, bias, shape, sched=None, y=None):
 # The forms are tt.h's.  Values are torch.float8_e4m3fn, scales float32; a tensor of another type, size, layout or device than
 # the shape says is TT_ERR_BAD_ARG.  Outputs and workspaces that the caller does not give are allocated.
 TT_FP8_BLOCK = 128
-TT_FP8_DIRECT, TT_FP8_TILES, TT_FP8_BLOCKS = range(3)
+TT_FP8_STREAM, TT_FP8_TILES, TT_FP8_BLOCKS = range(3)
 TT_NORM_TWO_PASS, TT_NORM_ONE_PASS = range(2)
 TT_ACT_NONE, TT_ACT_RELU, TT_ACT_RELU6, TT_ACT_GELU, TT_ACT_SILU = range(5)
 

@@ -19,44 +19,6 @@
 
 namespace tt {
 
-// Position of a row's 16-byte pieces in the LDS: piece c of row r lies at c ^ swizzle(r).  A fragment's 16 lanes read one piece of
-// 16 rows, which the swizzle spreads over all banks (256 bytes, two rows).
-//   rows of A: r, r + 1, ... r + 15;   rows of B: 8 (i / 4) + i % 4 (+ 4), i = 0 .. 15, so that the matrix cores leave eight
-//   consecutive columns of the result in a lane.
-__device__ __forceinline__ int a_swizzle(int r) { return (r >> 1) & 7; }
-__device__ __forceinline__ int b_swizzle(int r) { return ((r >> 1) & 1) | ((r >> 2) & 6); }
-
-__device__ __forceinline__ void load4_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint32_t byte_offset, uint32_t lds_addr)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-                 :
-                 : "s"(lds_addr), "v"(byte_offset), "s"(rsrc)
-                 : "memory", "m0");
-}
-
-// Eight consecutive columns of one row of the result.
-template <int DT> __device__ __forceinline__ void store_eight(void *out, int64_t at, const float (&v)[8], int count);
-template <> __device__ __forceinline__ void store_eight<TT_BF16>(void *out, int64_t at, const float (&v)[8], int count)
-{
-    const u32x4 r = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-    store_piece<TT_BF16>(out, at, r, count);
-}
-template <> __device__ __forceinline__ void store_eight<TT_F32>(void *out, int64_t at, const float (&v)[8], int count)
-{
-    store_piece<TT_F32>(out, at, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, min(count, 4));
-    if (count > 4)
-        store_piece<TT_F32>(out, at + 4, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])}, count - 4);
-}
-template <int DT> __device__ __forceinline__ void load_eight(float (&v)[8], const void *p, int64_t at, int count)
-{
-#pragma unroll
-    for (int h = 0; h < 8; h += ElemOf<DT>::CH) {
-        const u32x4 r = count > h ? load_piece<DT>(p, at + h, count - h) : u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int e = 0; e < ElemOf<DT>::CH; ++e) v[h + e] = element_of<DT>(r, e);
-    }
-}
-
 struct Fp8Block {
     static constexpr int BM = 256, BN = 256, THREADS = 512, STEP = 64, NL = 2; // STEP: rows between the NL loads of a thread
     static constexpr int ROW = kFp8Block, REGION = 128 * ROW, SLICE = 4 * REGION;
@@ -64,7 +26,7 @@ struct Fp8Block {
     static constexpr int BAND = 4;
 };
 
-template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kernel(const ProductArgs g, int blocks_m, int blocks_n)
+template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kernel(const ProductArgs g)
 {
     using S = Fp8Block;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -74,17 +36,9 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
     const int team = wave >> 2;
     const int wm = team, wn = wave & 3; // 64-row strip of every region of A, 32-row strip of every region of B
 
-    // block of this workgroup: a contiguous run per XCD, in bands of four block rows (see contract_block)
     int m0, n0;
-    {
-        const int total = blocks_m * blocks_n, wg = (int)blockIdx.x;
-        const int per = total / kXcds, rem = total % kXcds, x = wg % kXcds;
-        const int L = x * per + min(x, rem) + wg / kXcds;
-        const int band = L / (S::BAND * blocks_n), at = L - band * S::BAND * blocks_n;
-        const int high = min(S::BAND, blocks_m - band * S::BAND);
-        m0 = (band * S::BAND + at % high) * S::BM;
-        n0 = at / high * S::BN;
-    }
+    place_of_tile((int)blockIdx.x, g.tiles_m, g.tiles_n, S::BAND, &m0, &n0);
+    m0 *= S::BM, n0 *= S::BN;
     const int64_t batch = blockIdx.y;
     const int kb = g.kb;
     const uint32_t kp = (uint32_t)kb * kFp8Block;
@@ -126,22 +80,18 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
     const int a_row = wm * 64 + lane_r, b_row = wn * 32 + lane_r / 4 * 8 + lane_r % 4;
     // (rows 16 further have A's swizzle unchanged, rows 4 further B's)
     const int a_from = a_row * S::ROW + (lane_g ^ a_swizzle(a_row)) * 16, b_from = b_row * S::ROW + (lane_g ^ b_swizzle(b_row)) * 16;
-    Fragment af[4], bf[2][2];
-    auto read_a = [&](int h, int buffer) {
-        const unsigned char *const from = smem + buffer * S::SLICE + h * S::REGION;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            af[i].lo = *reinterpret_cast<const u32x4 *>(from + i * 16 * S::ROW + a_from);
-            af[i].hi = *reinterpret_cast<const u32x4 *>(from + i * 16 * S::ROW + (a_from ^ 64));
-        }
+    using P = BlockProduct<TT_BF16>;
+    P::Operand af[4], bf[2][2];
+    auto fragment = [&](const unsigned char *from, int at) {
+        return P::operand({*reinterpret_cast<const u32x4 *>(from + at), *reinterpret_cast<const u32x4 *>(from + (at ^ 64))});
     };
-    auto read_b = [&](Fragment (&to)[2], int h, int buffer) {
-        const unsigned char *const from = smem + buffer * S::SLICE + (2 + h) * S::REGION;
+    auto read_a = [&](int h, int buffer) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            to[j].lo = *reinterpret_cast<const u32x4 *>(from + j * 4 * S::ROW + b_from);
-            to[j].hi = *reinterpret_cast<const u32x4 *>(from + j * 4 * S::ROW + (b_from ^ 64));
-        }
+        for (int i = 0; i < 4; ++i) af[i] = fragment(smem + buffer * S::SLICE + h * S::REGION + i * 16 * S::ROW, a_from);
+    };
+    auto read_b = [&](P::Operand (&to)[2], int h, int buffer) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) to[j] = fragment(smem + buffer * S::SLICE + (2 + h) * S::REGION + j * 4 * S::ROW, b_from);
     };
     auto swap_teams = [&]() {
         asm volatile("" ::: "memory");
@@ -172,11 +122,11 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
             c[x / 2][x % 2][e] = fmaf(part[x][e], B_ROWS == 1 ? sa[x / 2] * sb[(x % 2 * 4 + e) % (B_ROWS == 1 ? 8 : 1)] : sa[x / 2], c[x / 2][x % 2][e]);
     };
     constexpr int LAG = 2; // matrix instructions issued before the first one's products are used
-    auto multiply = [&](f32x4 (&c)[4][2], const Fragment (&b)[2]) {
+    auto multiply = [&](f32x4 (&c)[4][2], const P::Operand (&b)[2]) {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
-            part[x] = BlockProduct<TT_BF16>::run(b[x % 2], af[x / 2]);
+            part[x] = P::run(b[x % 2], af[x / 2]);
             __builtin_amdgcn_sched_barrier(0);
             if (x >= LAG) accumulate(c, x - LAG);
             __builtin_amdgcn_sched_barrier(0);
@@ -197,7 +147,7 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
     if (team == 1) swap_teams(); // team 1 runs one turn behind
 
     // `buffer`: t mod 2, a constant
-    auto step = [&](int t, int buffer, Fragment (&b0)[2], Fragment (&b1)[2]) {
+    auto step = [&](int t, int buffer, P::Operand (&b0)[2], P::Operand (&b1)[2]) {
         // phase 0
         read_a(0, buffer);
         request_b(1, t + 1, buffer ^ 1);
@@ -256,8 +206,8 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
                 if (m >= g.M || n >= g.N) continue;
                 float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = acc[h][k][i][e / 4][e % 4] + bias[e];
-                apply_act_all<8>(v, g.act);
+                for (int e = 0; e < 8; ++e) v[e] = acc[h][k][i][e / 4][e % 4];
+                finish_results<8>(v, bias, g.act);
                 store_eight<TT_BF16>(g.out, (batch * g.M + m) * g.N + n, v, g.N - n);
             }
     }

@@ -1,10 +1,14 @@
 // Products of matrices held in 8 bits, entry points and launch rule.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "fp8_block.hip.h"
 
 namespace tt {
 namespace {
+
+constexpr int kStreamRows = 64; // of A at most
 
 int plan_of(const tt_fp8_shape &s, tt_fp8_launch *l)
 {
@@ -12,44 +16,67 @@ int plan_of(const tt_fp8_shape &s, tt_fp8_launch *l)
     if (s.dtype != TT_F32 && s.dtype != TT_BF16) return TT_ERR_BAD_ARG;
     *l = tt_fp8_launch{};
     if (s.k > kFp8LargestK || s.batch > 65535) return TT_ERR_UNSUPPORTED;
-    const int64_t blocks_m = (s.m + 255ll) / 256, blocks_n = (s.n + 255ll) / 256;
-    if (s.dtype == TT_BF16 && blocks_m * blocks_n * s.batch >= compute_units() / 2) {
-        l->kernel = TT_FP8_BLOCKS;
-        l->tile_m = l->tile_n = 256;
-        l->split_k = 1;
-        if (blocks_m * blocks_n > INT32_MAX) return TT_ERR_UNSUPPORTED;
-        l->grid = (int32_t)(blocks_m * blocks_n);
-        l->block = Fp8Block::THREADS;
-        l->lds_bytes = Fp8Block::LDS;
-        return TT_OK;
-    }
-    l->kernel = TT_FP8_DIRECT;
-    l->tile_m = l->tile_n = 16;
-    l->split_k = 1;
-    const int64_t grid = ((s.m + 15ll) / 16) * ((s.n + 15ll) / 16);
-    if (grid > INT32_MAX) return TT_ERR_UNSUPPORTED;
+    const int64_t kb = fp8_blocks(s.k), cus = compute_units();
+    auto tiles = [&](int64_t tm, int64_t tn) { return ((s.m + tm - 1) / tm) * ((s.n + tn - 1) / tn); };
+    auto in = [&](int kernel, int tm, int tn, int block, int lds) {
+        l->kernel = kernel, l->tile_m = tm, l->tile_n = tn, l->split_k = 1, l->block = block, l->lds_bytes = lds;
+    };
+    if (s.dtype == TT_BF16 && tiles(256, 256) * s.batch >= cus / 2)
+        in(TT_FP8_BLOCKS, 256, 256, Fp8Block::THREADS, Fp8Block::LDS);
+    else if (s.m <= kStreamRows)
+        in(TT_FP8_STREAM, s.m <= 16 ? 16 : s.m <= 32 ? 32 : 64, 16, 512, 0);
+    else if (tiles(128, 128) * s.batch >= cus)
+        in(TT_FP8_TILES, 128, 128, 256, Tiles<128, 128>::LDS);
+    else
+        in(TT_FP8_TILES, 64, 64, 256, Tiles<64, 64>::LDS);
+    const int64_t grid = tiles(l->tile_m, l->tile_n);
+    if (grid * l->block > INT32_MAX) return TT_ERR_UNSUPPORTED;
     l->grid = (int32_t)grid;
-    l->block = 64;
+    if (l->kernel == TT_FP8_TILES && grid * s.batch * 2 <= cus) {
+        const int64_t splits = std::min<int64_t>(kb / 4, cus / (grid * s.batch));
+        if (splits > 1) {
+            const int64_t steps = (kb + splits - 1) / splits;
+            l->split_k = (int32_t)((kb + steps - 1) / steps);
+            l->workspace_bytes = (int64_t)l->split_k * s.batch * s.m * s.n * 4;
+        }
+    }
     return TT_OK;
 }
 
-template <int B_ROWS> int launch_blocks(const ProductArgs &g, const tt_fp8_launch &l, void *stream)
+int launched(const char *what)
 {
-    auto kern = product_block_kernel<B_ROWS>;
-    static DynamicLdsLimit limit;
-    if (const int rc = limit.raise_to(reinterpret_cast<const void *>(kern), l.lds_bytes); rc != TT_OK) return rc;
-    hipLaunchKernelGGL(kern, dim3(l.grid, g.batch), dim3(l.block), l.lds_bytes, static_cast<hipStream_t>(stream), g, (g.M + 255) / 256, (g.N + 255) / 256);
     const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? TT_OK : note_hip_error((int)e, "product_block_kernel launch");
+    return e == hipSuccess ? TT_OK : note_hip_error((int)e, what);
 }
 
-template <int DT> int launch(const ProductArgs &g, const tt_fp8_launch &l, void *stream)
+// (a kernel per instance, so that its limit is raised once)
+template <auto KERNEL> int launch_kernel(const ProductArgs &g, const tt_fp8_launch &l, void *stream)
 {
+    static DynamicLdsLimit limit;
+    if (const int rc = limit.raise_to(reinterpret_cast<const void *>(KERNEL), l.lds_bytes); rc != TT_OK) return rc;
+    hipLaunchKernelGGL(KERNEL, dim3(l.grid, g.batch, l.split_k), dim3(l.block), l.lds_bytes, static_cast<hipStream_t>(stream), g);
+    return launched("8-bit product launch");
+}
+
+template <int DT, int B_ROWS> int launch(ProductArgs &g, const tt_fp8_launch &l, void *stream)
+{
+    g.tiles_m = (g.M + l.tile_m - 1) / l.tile_m, g.tiles_n = (g.N + l.tile_n - 1) / l.tile_n;
+    g.splits = l.split_k, g.split_steps = (g.kb + l.split_k - 1) / l.split_k;
+    if (l.kernel == TT_FP8_STREAM) {
+        switch (l.tile_m) {
+        case 16: return launch_kernel<product_stream_kernel<DT, 1>>(g, l, stream);
+        case 32: return launch_kernel<product_stream_kernel<DT, 2>>(g, l, stream);
+        default: return launch_kernel<product_stream_kernel<DT, 4>>(g, l, stream);
+        }
+    }
     if constexpr (DT == TT_BF16)
-        if (l.kernel == TT_FP8_BLOCKS) return g.b_rows == 1 ? launch_blocks<1>(g, l, stream) : launch_blocks<kFp8Block>(g, l, stream);
-    hipLaunchKernelGGL((product_direct_kernel<DT>), dim3(l.grid, g.batch), dim3(l.block), 0, static_cast<hipStream_t>(stream), g);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? TT_OK : note_hip_error((int)e, "product_direct_kernel launch");
+        if (l.kernel == TT_FP8_BLOCKS) return launch_kernel<product_block_kernel<B_ROWS>>(g, l, stream);
+    const int rc = l.tile_m == 128 ? launch_kernel<product_tile_kernel<DT, 128, 128, B_ROWS>>(g, l, stream)
+                                   : launch_kernel<product_tile_kernel<DT, 64, 64, B_ROWS>>(g, l, stream);
+    if (rc != TT_OK || l.split_k == 1) return rc;
+    const int64_t threads = (int64_t)g.batch * g.M * ((g.N + 7) / 8);
+    hipLaunchKernelGGL((product_reduce_kernel<DT>), dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), g);
+    return launched("product_reduce_kernel launch");
 }
 
 int run(const void *a, const float *a_scale, const void *b, const float *b_scale, const void *bias, void *c,
@@ -68,7 +95,9 @@ int run(const void *a, const float *a_scale, const void *b, const float *b_scale
     g.batch = shape->batch, g.M = shape->m, g.N = shape->n, g.kb = (int32_t)fp8_blocks(shape->k);
     g.b_rows = shape->b_rows, g.act = act;
     g.b_scale_row = (shape->n + shape->b_rows - 1) / shape->b_rows;
-    return shape->dtype == TT_F32 ? launch<TT_F32>(g, l, stream) : launch<TT_BF16>(g, l, stream);
+    g.ws = static_cast<float *>(ws);
+    if (g.b_rows == 1) return shape->dtype == TT_F32 ? launch<TT_F32, 1>(g, l, stream) : launch<TT_BF16, 1>(g, l, stream);
+    return shape->dtype == TT_F32 ? launch<TT_F32, kFp8Block>(g, l, stream) : launch<TT_BF16, kFp8Block>(g, l, stream);
 }
 
 } // namespace
