@@ -328,9 +328,9 @@ int tt_dwconv(const void *x, const void *w, const void *bias, void *y, const tt_
  * stands for value[r][j] * scale[j / 128][r / block_rows].  A batch is that many such matrices one behind the other, values and
  * scales apart.
  *
- * tt_quantize_fp8: x [batch, rows, cols] of `dtype` into that form.  For every block a = max(max |x|, 2^-100), scale = a / 448,
- * value = x * (448 / a), all in float32, rounded to nearest even.  A block that holds an infinity or a NaN has that as its
- * scale, and everything computed from the block is NaN.
+ * tt_quantize_fp8: x [batch, rows, cols] of `dtype` into that form.  For every block a = max(max |x|, 2^-100), scale = a / 448 rounded
+ * to float32, and value = x * 448 / a rounded once, to the nearest e4m3, ties to even.  A block that holds an infinity or a NaN has
+ * that as its scale, and everything computed from the block is NaN.
  */
 #define TT_FP8_BLOCK 128
 typedef struct tt_quant_shape {
@@ -377,7 +377,8 @@ int tt_batch_matmul_fp8(const void *a, const float *a_scale, const void *b, cons
  * y = act((x - mean) / sqrt(var + eps) * gamma[c] + beta[c]), mean and (biased) variance over the pixels and channels of an
  * (image, group), in float32 from differences to the mean.  gamma, beta [c] of x's type, or NULL for ones and zeros.
  * tt_group_norm_act_fp8 writes act's float32 values as a matrix held in 8 bits instead, [n * h * w, c] with a scale per pixel
- * and 128 channels: the left operand of tt_dense_fp8 for a pointwise convolution or dense layer.
+ * and 128 channels (its values are x * (448 / a) in float32 before their last rounding): the left operand of tt_dense_fp8 for a
+ * pointwise convolution or dense layer.  A NaN stays one through every activation, here and in tt_dense_fp8.
  * Partial statistics live in the workspace: tt_norm_plan says how large it is (none: 0).  eps >= 0.
  */
 typedef enum tt_act { TT_ACT_NONE = 0, TT_ACT_RELU = 1, TT_ACT_RELU6 = 2, TT_ACT_GELU = 3, TT_ACT_SILU = 4 } tt_act;

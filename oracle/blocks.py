@@ -35,7 +35,8 @@ def e4m3(v):
 def quantize(x, group):
     """x [batch, rows, cols] (float32 values) -> (values [batch, rows, kp], scales [batch, kb, row blocks]).
 
-    The rule is stated in float32 (two divisions and one product, each rounded once), so this is bit for bit."""
+    A scale is rounded once, to float32, and so is a value, x * 448 / largest to e4m3, so this is bit for bit: a quotient of float32
+    numbers that is no midpoint of e4m3 is further from one than a rounding in 64 bits."""
     x = np.asarray(x, np.float32)
     batch, rows, cols = x.shape
     kb, rb = -(-cols // BLOCK), -(-rows // group)
@@ -50,7 +51,7 @@ def quantize(x, group):
                     top = np.max(np.abs(x[cut]))  # (numpy's max is NaN where one is)
                     top = f32(2.0 ** -100) if top < f32(2.0 ** -100) else top
                     scale[i, b, r] = top / f32(448.0)
-                    q[cut] = e4m3((x[cut] * (f32(448.0) / top)).astype(f32))
+                    q[cut] = e4m3(x[cut].astype(np.float64) * 448.0 / np.float64(top))
     return q, scale
 
 

@@ -10,7 +10,7 @@
 //   request    B1 (t + 1)   A1 (t + 1)   A0 (t + 2)   B0 (t + 2), scales (t + 2)          (step t, buffer t mod 2)
 //
 // What is new is the scaling.  A matrix instruction starts from zero, and its four sums a lane go into the accumulators by FMAs
-// two instructions later, in issue slots that the matrix cores leave free (32 cycles an instruction, 16 of FMAs); the last two
+// three instructions later, in issue slots that the matrix cores leave free (32 cycles an instruction, 16 of FMAs); the last three
 // of a turn are taken in the next reading turn, so that no wave waits for a product's latency.
 // A step's scales, 256 of A and as many of B, come into the LDS with the operands, in a ring of four.
 #pragma once
@@ -83,7 +83,7 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
     using P = BlockProduct<TT_BF16>;
     P::Operand af[4], bf[2][2];
     auto fragment = [&](const unsigned char *from, int at) {
-        return P::operand({*reinterpret_cast<const u32x4 *>(from + at), *reinterpret_cast<const u32x4 *>(from + (at ^ 64))});
+        return P::hold({*reinterpret_cast<const u32x4 *>(from + at), *reinterpret_cast<const u32x4 *>(from + (at ^ 64))});
     };
     auto read_a = [&](int h, int buffer) {
 #pragma unroll
@@ -121,7 +121,7 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
         for (int e = 0; e < 4; ++e)
             c[x / 2][x % 2][e] = fmaf(part[x][e], B_ROWS == 1 ? sa[x / 2] * sb[(x % 2 * 4 + e) % (B_ROWS == 1 ? 8 : 1)] : sa[x / 2], c[x / 2][x % 2][e]);
     };
-    constexpr int LAG = 2; // matrix instructions issued before the first one's products are used
+    constexpr int LAG = 3; // matrix instructions issued before the first one's products are used
     auto multiply = [&](f32x4 (&c)[4][2], const P::Operand (&b)[2]) {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll

@@ -18,6 +18,21 @@ constexpr uint32_t kFp8Smallest = (127u - 100u) << 23; // 2^-100: below it 448 /
 // and the remainder of the quotient they are nine.  Checked for every mantissa of a: both are the rounded quotients.
 struct Fp8Scale {
     float scale, factor;
+    float rest; // 448 / a - factor, to 24 bits
+    // x * 448 / a, to be rounded to e4m3 as if it had never been rounded before.
+    // bf16 x: rounded to float32 once, instead of factor and product each.  An 8-bit by 3-bit product over an 8-bit one that is no
+    // midpoint of e4m3 is 2^-13 of itself away from one, so that no second rounding lands there.
+    // float32 x: rounded to the odd neighbour where it is not exact, which no midpoint is.  (What is left over is itself off by some
+    // 2^-47 of y; where y is a midpoint and not exact it is at least 2^-30 of it, a 24-bit product's distance from a 29-bit one.)
+    template <int DT> __device__ __forceinline__ float value(float x) const
+    {
+#pragma clang fp contract(off) // (v is the rounded product, also where it is added to)
+        const float v = x * factor, e = fmaf(x, rest, fmaf(x, factor, -v)), y = v + e;
+        if constexpr (DT == TT_BF16) return y;
+        const float over = e - (y - v);
+        const uint32_t b = __float_as_uint(y), away = (b ^ __float_as_uint(over)) >> 31;
+        return fabsf(over) > fabsf(y) * 0x1p-40f && (b & 1u) == 0u ? __uint_as_float(b + 1u - 2u * away) : y;
+    }
 };
 __device__ __forceinline__ Fp8Scale fp8_scale(uint32_t largest)
 {
@@ -29,8 +44,11 @@ __device__ __forceinline__ Fp8Scale fp8_scale(uint32_t largest)
         s.scale = fmaf(fmaf(-448.0f, q, a), R, q);
         const float r0 = __builtin_amdgcn_rcpf(a), r = fmaf(fmaf(-a, r0, 1.0f), r0, r0), f = 448.0f * r;
         s.factor = fmaf(fmaf(-a, f, 448.0f), r, f);
-    } else
+        s.rest = fmaf(-a, s.factor, 448.0f) * r;
+    } else {
         s.scale = a / 448.0f, s.factor = 448.0f / a;
+        s.rest = largest < 0x7f800000u ? fmaf(-a, s.factor, 448.0f) / a : 0.0f;
+    }
     return s;
 }
 // The largest magnitude of values, two at a time: as signed integers the positive ones are in order, as unsigned ones the negative
@@ -53,7 +71,7 @@ __device__ __forceinline__ uint32_t largest_of_16_lanes(uint32_t v)
     v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, false));
     return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, false));
 }
-// Four values to nearest even.  |x| <= a keeps x * factor within 448 * (1 + 2^-23), which rounds to 448: nothing overflows.
+// Four values to nearest even.  |x| <= a keeps them within 448 * (1 + 2^-23), which rounds to 448: nothing overflows.
 __device__ __forceinline__ uint32_t pack_fp8x4(float a, float b, float c, float d)
 {
     const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);

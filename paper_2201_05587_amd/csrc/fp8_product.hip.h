@@ -33,12 +33,15 @@ struct Fragment {
     u32x4 lo, hi;
 };
 
-// The sums of 128 products, 16 rows of B by 16 rows of A, of operands in the form that the matrix cores take.
+// The sums of 128 products, 16 rows of B by 16 rows of A, of operands in the form that the matrix cores take (Held: as they wait in
+// registers).
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 template <int DT> struct BlockProduct;
 template <> struct BlockProduct<TT_BF16> {
     using Operand = i32x8;
-    static __device__ __forceinline__ Operand operand(const Fragment &f)
+    using Held = i32x8;
+    static __device__ __forceinline__ Operand operand(const Held &h) { return h; }
+    static __device__ __forceinline__ Held hold(const Fragment &f)
     {
         return __builtin_shufflevector(__builtin_bit_cast(i32x4, f.lo), __builtin_bit_cast(i32x4, f.hi), 0, 1, 2, 3, 4, 5, 6, 7);
     }
@@ -58,6 +61,8 @@ template <> struct BlockProduct<TT_F32> {
     struct Operand {
         bf16x8 v[4];
     };
+    using Held = Fragment;
+    static __device__ __forceinline__ Held hold(const Fragment &f) { return f; }
     static __device__ __forceinline__ Operand operand(const Fragment &f)
     {
         return {{widen_fp8(f.lo[0], f.lo[1]), widen_fp8(f.lo[2], f.lo[3]), widen_fp8(f.hi[0], f.hi[1]), widen_fp8(f.hi[2], f.hi[3])}};
@@ -142,7 +147,7 @@ __device__ __forceinline__ void place_of_tile(int wg, int tiles_m, int tiles_n, 
 // they are, UNROLL steps of loads in flight, and the waves' sums meet in the LDS.  What is read is B, once, and A by every
 // workgroup (from the L2): the kernel for a token or a few, whose time is B's bytes.
 template <int MS> struct Stream {
-    static constexpr int WAVES = 8, UNROLL = MS <= 2 ? 4 : 2, LDS = WAVES * MS * 64 * 16;
+    static constexpr int WAVES = 8, UNROLL = 4;
 };
 template <int DT, int MS> __global__ void __launch_bounds__(512) product_stream_kernel(const ProductArgs g)
 {
@@ -185,10 +190,10 @@ template <int DT, int MS> __global__ void __launch_bounds__(512) product_stream_
 #pragma unroll
         for (int u = 0; u < S::UNROLL; ++u) {
             if (first + u * S::WAVES >= g.kb) break;
-            const typename P::Operand bx = P::operand(x[u]);
+            const typename P::Operand bx = P::operand(P::hold(x[u]));
 #pragma unroll
             for (int i = 0; i < MS; ++i) {
-                const f32x4 p = P::run(bx, P::operand(y[u][i]));
+                const f32x4 p = P::run(bx, P::operand(P::hold(y[u][i])));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[i][e] = fmaf(p[e], sa[u][i] * sb[u][e], sum[i][e]);
             }
@@ -221,16 +226,19 @@ template <int DT, int MS> __global__ void __launch_bounds__(512) product_stream_
 
 // ---- tiles -----------------------------------------------------------------------------------------------------------
 // TM x TN outputs a workgroup of four waves (2 x 2), steps of the reduction through a ring of LDS buffers that asynchronous loads
-// fill three steps ahead, one barrier a step.  Both float32 and bf16 results, and splits of the reduction where the tiles are too few
-// for the chip: their sums go to the workspace, and product_reduce_kernel adds them.
+// fill two to three steps ahead, one barrier a step.  A workgroup of 128 x 128 has a CU to itself, and its waves read the next step's
+// fragments before they multiply the present one's; of 64 x 64 a CU has three, which run past each other.
+// Both float32 and bf16 results, and splits of the reduction where the tiles are too few for the chip: their sums go to the
+// workspace, and product_reduce_kernel adds them.
 template <int TM, int TN> struct Tiles {
-    static constexpr int THREADS = 256, RING = 4, WM = TM / 2, WN = TN / 2, MI = WM / 16, NJ = WN / 16;
+    static constexpr bool AHEAD = TM * TN > 64 * 64; // fragments of the next step are read before the present one is multiplied
+    static constexpr int THREADS = 256, RING = AHEAD ? 4 : 3, WM = TM / 2, WN = TN / 2, MI = WM / 16, NJ = WN / 16;
     static constexpr int A_BYTES = TM * kFp8Block, B_BYTES = TN * kFp8Block, SCALES = 1024, STAGE = A_BYTES + B_BYTES + SCALES;
     static constexpr int LOADS = (TM + TN) / 32 + 1; // of a thread and step: 16-byte items, and one scale
     static constexpr int LDS = RING * STAGE, BAND = 8;
     static_assert(TM + TN <= THREADS && WN % 32 == 0, "");
 };
-template <int DT, int TM, int TN, int B_ROWS> __global__ void __launch_bounds__(256) product_tile_kernel(const ProductArgs g)
+template <int DT, int TM, int TN, int B_ROWS> __global__ void __launch_bounds__(256, 2) product_tile_kernel(const ProductArgs g)
 {
     using S = Tiles<TM, TN>;
     using P = BlockProduct<DT>;
@@ -273,43 +281,106 @@ template <int DT, int TM, int TN, int B_ROWS> __global__ void __launch_bounds__(
     const int lane_r = lane % 16, lane_g = lane / 16;
     const int a_row = wm * S::WM + lane_r, b_row = wn * S::WN + lane_r / 4 * 8 + lane_r % 4;
     const int a_from = a_row * kFp8Block + (lane_g ^ a_swizzle(a_row)) * 16, b_from = S::A_BYTES + b_row * kFp8Block + (lane_g ^ b_swizzle(b_row)) * 16;
-#pragma unroll
-    for (int t = 0; t < S::RING - 1; ++t) request(begin + t);
-    for (int t = begin; t < end; ++t) {
-        wait_loads_outstanding<(S::RING - 2) * S::LOADS>(); // step t has landed
-        __syncthreads();                                    // ... for every wave, and all have read step t - 1
-        request(t + S::RING - 1);
+    // what a wave multiplies in a step
+    struct Step {
+        typename P::Held a[S::MI], b[S::NJ];
+    };
+    auto fragment = [&](const unsigned char *from, int at) {
+        return P::hold({*reinterpret_cast<const u32x4 *>(from + at), *reinterpret_cast<const u32x4 *>(from + (at ^ 64))});
+    };
+    auto read = [&](Step &s, int t) {
         const unsigned char *const from = smem + (t % S::RING) * S::STAGE;
-        const float *const scales = reinterpret_cast<const float *>(from + S::A_BYTES + S::B_BYTES);
-        typename P::Operand af[S::MI];
-        float sa[S::MI];
-        const float sb0 = scales[TM + wn * S::WN];
 #pragma unroll
-        for (int i = 0; i < S::MI; ++i) {
-            Fragment f;
-            f.lo = *reinterpret_cast<const u32x4 *>(from + a_from + i * 16 * kFp8Block);
-            f.hi = *reinterpret_cast<const u32x4 *>(from + (a_from ^ 64) + i * 16 * kFp8Block);
-            af[i] = P::operand(f);
-            sa[i] = scales[a_row + i * 16];
-            if (B_ROWS > 1) sa[i] *= sb0;
+        for (int i = 0; i < S::MI; ++i) s.a[i] = fragment(from + i * 16 * kFp8Block, a_from);
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) s.b[j] = fragment(from + (j / 2 * 32 + j % 2 * 4) * kFp8Block, b_from); // (the same swizzle)
+    };
+    // the scales of step t: of the lane's rows of A (times that of B, where it is one), and of its four rows of B's block j
+    const int a_scale_at = S::A_BYTES + S::B_BYTES + 4 * a_row, b_scale_at = S::A_BYTES + S::B_BYTES + 4 * (TM + wn * S::WN + lane_g * 8);
+    auto read_scales = [&](float (&sa)[S::MI], f32x4 &sb, int t) {
+        const unsigned char *const from = smem + (t % S::RING) * S::STAGE;
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i) sa[i] = *reinterpret_cast<const float *>(from + a_scale_at + i * 64);
+        if constexpr (B_ROWS == 1)
+            sb = *reinterpret_cast<const f32x4 *>(from + b_scale_at);
+        else
+            sb[0] = *reinterpret_cast<const float *>(from + b_scale_at);
+    };
+    auto multiply = [&](const Step &s, float (&sa)[S::MI], f32x4 sb, int t) {
+        constexpr int COUNT = S::MI * S::NJ, LAG = COUNT < 8 ? 2 : 3; // matrix instructions issued before the first one's products are used
+        const unsigned char *const from = smem + (t % S::RING) * S::STAGE + b_scale_at;
+        if constexpr (B_ROWS > 1) {
+#pragma unroll
+            for (int i = 0; i < S::MI; ++i) sa[i] *= sb[0];
         }
+        f32x4 part[COUNT], sb_next = sb;
+        auto accumulate = [&](int x) {
+            const int i = x % S::MI, j = x / S::MI;
+            if (B_ROWS == 1 && i == 0) { // the next four rows' scales a block ahead
+                sb = sb_next;
+                if (j + 1 < S::NJ) sb_next = *reinterpret_cast<const f32x4 *>(from + 4 * ((j + 1) / 2 * 32 + (j + 1) % 2 * 4));
+            }
 #pragma unroll
-        for (int j = 0; j < S::NJ; ++j) {
-            Fragment f; // rows 32 (j / 2) + 4 (j % 2) further have the same swizzle
-            const int further = (j / 2 * 32 + j % 2 * 4) * kFp8Block;
-            f.lo = *reinterpret_cast<const u32x4 *>(from + b_from + further);
-            f.hi = *reinterpret_cast<const u32x4 *>(from + (b_from ^ 64) + further);
-            const typename P::Operand bf = P::operand(f);
-            f32x4 sb = {1.0f, 1.0f, 1.0f, 1.0f};
-            if (B_ROWS == 1) sb = *reinterpret_cast<const f32x4 *>(scales + TM + wn * S::WN + j / 2 * 32 + lane_g * 8 + j % 2 * 4);
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[x][e], B_ROWS == 1 ? sa[i] * sb[e] : sa[i], acc[i][j][e]);
+            asm volatile("" : "+v"(acc[i][j])); // (keeps the FMAs here, between the matrix instructions)
+        };
+        if constexpr (DT == TT_BF16) {
 #pragma unroll
-            for (int i = 0; i < S::MI; ++i) {
-                const f32x4 p = P::run(bf, af[i]);
+            for (int x = 0; x < COUNT; ++x) {
+                part[x] = P::run(P::operand(s.b[x / S::MI]), P::operand(s.a[x % S::MI]));
+                __builtin_amdgcn_sched_barrier(0);
+                if (x >= LAG) accumulate(x - LAG);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], B_ROWS == 1 ? sa[i] * sb[e] : sa[i], acc[i][j][e]);
+            for (int x = COUNT - LAG; x < COUNT; ++x) accumulate(x);
+        } else {
+            typename P::Operand a[S::MI];
+#pragma unroll
+            for (int i = 0; i < S::MI; ++i) a[i] = P::operand(s.a[i]);
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j) {
+                const typename P::Operand b = P::operand(s.b[j]);
+#pragma unroll
+                for (int i = 0; i < S::MI; ++i) part[j * S::MI + i] = P::run(b, a[i]);
+#pragma unroll
+                for (int i = 0; i < S::MI; ++i) accumulate(j * S::MI + i);
             }
         }
-    }
+    };
+#pragma unroll
+    for (int t = 0; t < S::RING - 1; ++t) request(begin + t);
+    if constexpr (S::AHEAD) {
+        wait_loads_outstanding<(S::RING - 2) * S::LOADS>();
+        __syncthreads();
+        Step now, next;
+        read(now, begin);
+        auto step = [&](int t, const Step &now, Step &next) {
+            float sa[S::MI];
+            f32x4 sb;
+            wait_loads_outstanding<(S::RING - 3) * S::LOADS>(); // step t + 1 has landed
+            __syncthreads();                                    // ... for every wave, and all have multiplied step t - 1
+            request(t + S::RING - 1);
+            read_scales(sa, sb, t);
+            read(next, t + 1); // (past the end: what the requests past the end left, zeros)
+            multiply(now, sa, sb, t);
+        };
+        for (int t = begin; t < end; t += 2) {
+            step(t, now, next);
+            if (t + 1 < end) step(t + 1, next, now);
+        }
+    } else
+        for (int t = begin; t < end; ++t) {
+            Step now;
+            float sa[S::MI];
+            f32x4 sb;
+            wait_loads_outstanding<(S::RING - 2) * S::LOADS>(); // step t has landed
+            __syncthreads();                                    // ... for every wave, and all have multiplied step t - 1
+            request(t + S::RING - 1);
+            read_scales(sa, sb, t);
+            read(now, t);
+            multiply(now, sa, sb, t);
+        }
     wait_loads_outstanding<0>(); // the requests past the end: nothing may still write the LDS when the workgroup ends
 #pragma unroll
     for (int jj = 0; jj < S::NJ / 2; ++jj) {
@@ -344,6 +415,7 @@ template <int DT> __global__ void __launch_bounds__(256) product_reduce_kernel(c
     const int64_t at = row * g.N + n, apart = (int64_t)g.batch * g.M * g.N;
     float v[8], bias[8] = {};
     load_eight<TT_F32>(v, g.ws, at, g.N - n);
+#pragma unroll 4
     for (int s = 1; s < g.splits; ++s) {
         float more[8];
         load_eight<TT_F32>(more, g.ws + s * apart, at, g.N - n);

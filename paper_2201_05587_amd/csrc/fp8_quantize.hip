@@ -39,10 +39,12 @@ template <int DT> struct EightColumns {
 #pragma unroll
         for (int e = 0; e < 8; e += 2) top.add((*this)[e], (*this)[e + 1]);
     }
-    __device__ __forceinline__ void store(uint8_t *to, float f) const
+    __device__ __forceinline__ void store(uint8_t *to, const Fp8Scale &s) const
     {
-        *reinterpret_cast<uint2 *>(to) = uint2{pack_fp8x4((*this)[0] * f, (*this)[1] * f, (*this)[2] * f, (*this)[3] * f),
-                                               pack_fp8x4((*this)[4] * f, (*this)[5] * f, (*this)[6] * f, (*this)[7] * f)};
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = s.value<DT>((*this)[e]);
+        *reinterpret_cast<uint2 *>(to) = uint2{pack_fp8x4(v[0], v[1], v[2], v[3]), pack_fp8x4(v[4], v[5], v[6], v[7])};
     }
 };
 
@@ -68,7 +70,7 @@ template <int DT, int R> __global__ void __launch_bounds__(256) quantize_rows_ke
         Largest top;
         x[i].largest(top);
         const Fp8Scale s = fp8_scale(largest_of_16_lanes(top.bits()));
-        x[i].store(g.q + (row0 + r) * g.kb * kFp8Block + col, s.factor);
+        x[i].store(g.q + (row0 + r) * g.kb * kFp8Block + col, s);
         if (tid % 16 == 0) scales[r][block - block0] = s.scale;
     }
     __syncthreads();
@@ -81,30 +83,33 @@ template <int DT, int R> __global__ void __launch_bounds__(256) quantize_rows_ke
     }
 }
 
-// A scale per 128 x 128: a block a workgroup, eight rows a thread.
-template <int DT> __global__ void __launch_bounds__(256) quantize_squares_kernel(const QuantizeArgs g)
+// A scale per 128 x 128: a block a workgroup, four rows a thread.
+template <int DT> __global__ void __launch_bounds__(512) quantize_squares_kernel(const QuantizeArgs g)
 {
-    __shared__ uint32_t tops[4];
+    constexpr int R = 4;
+    __shared__ uint32_t tops[8];
     const int tid = threadIdx.x;
     const int row_blocks = (g.rows + kFp8Block - 1) / kFp8Block;
     const int64_t batch = blockIdx.x / row_blocks, row_block = blockIdx.x % row_blocks;
     const int row = (int)row_block * kFp8Block + tid / 16, col = (int)blockIdx.y * kFp8Block + tid % 16 * 8;
-    EightColumns<DT> x[8];
+    EightColumns<DT> x[R];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i].load(g.x, (batch * g.rows + min(row + i * 16, g.rows - 1)) * g.cols + col, g.cols - col);
+    for (int i = 0; i < R; ++i) x[i].load(g.x, (batch * g.rows + min(row + i * 32, g.rows - 1)) * g.cols + col, g.cols - col);
     Largest largest; // (rows past the end are the last one again)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i].largest(largest);
+    for (int i = 0; i < R; ++i) x[i].largest(largest);
     uint32_t top = largest_of_16_lanes(largest.bits());
     top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
     if (tid % 64 == 0) tops[tid / 64] = top;
     __syncthreads();
-    const Fp8Scale s = fp8_scale(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = max(top, tops[w]);
+    const Fp8Scale s = fp8_scale(top);
     if (tid == 0) g.scale[(batch * g.kb + blockIdx.y) * row_blocks + row_block] = s.scale;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (row + i * 16 < g.rows) x[i].store(g.q + (batch * g.rows + row + i * 16) * g.kb * kFp8Block + col, s.factor);
+    for (int i = 0; i < R; ++i)
+        if (row + i * 32 < g.rows) x[i].store(g.q + (batch * g.rows + row + i * 32) * g.kb * kFp8Block + col, s);
 }
 
 template <int DT> int launch(const QuantizeArgs &g, const tt_quant_shape &s, void *stream)
@@ -124,7 +129,7 @@ template <int DT> int launch(const QuantizeArgs &g, const tt_quant_shape &s, voi
             hipLaunchKernelGGL((quantize_rows_kernel<DT, 1>), grid, dim3(256), 0, on, g, bits);
     } else {
         const dim3 grid((uint32_t)((s.rows + kFp8Block - 1) / kFp8Block * s.batch), (uint32_t)g.kb);
-        hipLaunchKernelGGL((quantize_squares_kernel<DT>), grid, dim3(256), 0, on, g);
+        hipLaunchKernelGGL((quantize_squares_kernel<DT>), grid, dim3(512), 0, on, g);
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? TT_OK : note_hip_error((int)e, "quantize kernel launch");

@@ -115,6 +115,28 @@ def test_quantize_what_is_not_finite_zero_or_tiny(group, dtype):
     assert np.array_equal(s.cpu().numpy(), want_s, equal_nan=True)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_quantize_rounds_once_next_to_the_midpoints(dtype):
+    """Rows whose elements lie on, or a step of their type beside, what the midpoints of e4m3 stand for."""
+    rng = np.random.default_rng(8)
+    td = api.torch_dtype(dtype)
+    values = np.arange(0, 127, dtype=np.uint8)
+    values = torch.from_numpy(values).view(E4M3).double().numpy()
+    mid = (values[1:] + values[:-1]) / 2
+    rows = []
+    for _ in range(200):
+        a = torch.tensor(float(np.exp(rng.uniform(-20, 20)))).to(td)
+        x = torch.from_numpy(mid[rng.permutation(len(mid))[:127]] * float(a) / 448.0).to(td)
+        bits = x.view(torch.int32 if dtype == F32 else torch.int16) + torch.from_numpy(rng.integers(-1, 2, len(x))).to(torch.int32 if dtype == F32 else torch.int16)
+        x = bits.view(td) * torch.from_numpy(rng.choice([-1.0, 1.0], len(x))).to(td)
+        rows.append(torch.cat([a[None], x.where(x.abs() <= a, a), torch.zeros(127 - len(x), dtype=td)]))
+    x = torch.stack(rows)[None]
+    want_q, want_s = B.quantize(x.float().numpy(), 1)
+    q, s = api.tt_quantize_fp8(x.cuda(), api.tt_quant_shape(1, 200, x.shape[2], 1, dtype))
+    assert np.array_equal(q.float().cpu().numpy(), want_q) and np.array_equal(s.cpu().numpy(), want_s)
+
+
 # ---- products ------------------------------------------------------------------------------------------------------
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 1000, 4096), (2, 130, 200), (7, 513, 1000), (16, 96, 129), (17, 48, 384), (33, 257, 640), (64, 256, 512),
          (65, 130, 127), (100, 1000, 300), (128, 128, 128), (129, 384, 1152), (200, 77, 2048), (255, 640, 256), (300, 300, 300), (640, 257, 513)]
