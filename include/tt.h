@@ -23,7 +23,8 @@
  *
  * Conventions of every entry point
  *   - plain C ABI; every function returns a tt_status (0 = TT_OK, negative = error);
- *   - pointers named x, w, bias, residual, y, a, b, c, ws and `out_dev` are DEVICE
+ *   - pointers named x, w, bias, residual, y, a, b, c, q, scale, x_scale, w_scale,
+ *     a_scale, b_scale, gamma, beta, ws and `out_dev` are DEVICE
  *     pointers, 16-byte aligned, owned by the caller; all other pointers are HOST
  *     pointers.  The library never allocates or frees device memory;
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  The
@@ -330,7 +331,8 @@ int tt_dwconv(const void *x, const void *w, const void *bias, void *y, const tt_
  *
  * tt_quantize_fp8: x [batch, rows, cols] of `dtype` into that form.  For every block a = max(max |x|, 2^-100), scale = a / 448 rounded
  * to float32, and value = x * 448 / a rounded once, to the nearest e4m3, ties to even.  A block that holds an infinity or a NaN has
- * that as its scale, and everything computed from the block is NaN.
+ * that as its scale, and everything computed from the block is NaN.  TT_ERR_UNSUPPORTED: 2^26 rows or more in all, or more than 2^22
+ * columns.
  */
 #define TT_FP8_BLOCK 128
 typedef struct tt_quant_shape {
@@ -350,14 +352,16 @@ int tt_quantize_fp8(const void *x, void *q, float *scale, const tt_quant_shape *
  *   tt_dense_fp8         classes TT_DENSE_ADD, TT_DENSE_BIAS_RELU, TT_DENSE_BIAS_GELU; batch 1; bias may be NULL
  *   tt_batch_matmul_fp8  no bias, no activation; any batch
  * They stand outside the schedule records: the library chooses the launch from the shape, tt_fp8_plan says which, and how large a
- * workspace it needs (none: 0).  1 <= k <= 2^22, and rows of outputs by their tile at most 2^31 - 1 workgroups (else
- * TT_ERR_UNSUPPORTED).
+ * workspace it needs (none: 0).  TT_ERR_UNSUPPORTED: k above 2^22, a batch above 65535, a matrix above 2^46 bytes, or more
+ * workgroups than a launch has.
  */
 typedef struct tt_fp8_shape {
     int32_t batch, m, n, k;
     int32_t b_rows; /* rows of b that share a scale: 1 or 128 */
     int32_t dtype;  /* tt_dtype of c and bias */
 } tt_fp8_shape;
+/* TT_FP8_STREAM: 16 rows of b past all of a (a few rows); TT_FP8_TILES: 64 x 64 or 128 x 128 outputs, the reduction in split_k
+ * parts (a second launch adds them); TT_FP8_BLOCKS: 256 x 256 */
 enum tt_fp8_kernel { TT_FP8_STREAM = 0, TT_FP8_TILES = 1, TT_FP8_BLOCKS = 2 };
 typedef struct tt_fp8_launch {
     int32_t kernel; /* tt_fp8_kernel */
@@ -379,18 +383,20 @@ int tt_batch_matmul_fp8(const void *a, const float *a_scale, const void *b, cons
  * tt_group_norm_act_fp8 writes act's float32 values as a matrix held in 8 bits instead, [n * h * w, c] with a scale per pixel
  * and 128 channels (its values are x * (448 / a) in float32 before their last rounding): the left operand of tt_dense_fp8 for a
  * pointwise convolution or dense layer.  A NaN stays one through every activation, here and in tt_dense_fp8.
- * Partial statistics live in the workspace: tt_norm_plan says how large it is (none: 0).  eps >= 0.
+ * Partial statistics live in the workspace: tt_norm_plan says how large it is (none: 0).  eps >= 0.  TT_ERR_UNSUPPORTED: more than
+ * 65535 images, 2^20 channels, 2^30 pixels of an image or 2^31 - 1 of all, or more workgroups than a launch has.
  */
 typedef enum tt_act { TT_ACT_NONE = 0, TT_ACT_RELU = 1, TT_ACT_RELU6 = 2, TT_ACT_GELU = 3, TT_ACT_SILU = 4 } tt_act;
 typedef struct tt_norm_shape {
     int32_t n, h, w, c, groups; /* groups divides c */
     int32_t dtype;              /* tt_dtype of x, gamma, beta, y */
 } tt_norm_shape;
+/* TT_NORM_TWO_PASS: statistics in one launch, results in a second; TT_NORM_ONE_PASS: an image's pixels in a workgroup's registers */
 enum tt_norm_kernel { TT_NORM_TWO_PASS = 0, TT_NORM_ONE_PASS = 1 };
 typedef struct tt_norm_launch {
     int32_t kernel; /* tt_norm_kernel */
     int32_t chunks; /* partial statistics of an (image, group) */
-    int32_t grid, block;
+    int32_t grid, block; /* grid: of one image, in the last launch */
     int64_t workspace_bytes;
 } tt_norm_launch;
 int tt_norm_plan(const tt_norm_shape *shape, int fp8, tt_norm_launch *launch);

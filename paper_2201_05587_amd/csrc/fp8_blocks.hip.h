@@ -11,8 +11,7 @@ TT_HD int64_t fp8_blocks(int64_t cols) { return (cols + kFp8Block - 1) / kFp8Blo
 
 // The largest magnitude of a block is found on the bits of |x|: as unsigned integers they are in the order of the magnitudes,
 // infinity above the finite values and NaN above infinity, where fmaxf would drop a NaN.
-__device__ __forceinline__ uint32_t magnitude_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-constexpr uint32_t kFp8Smallest = (127u - 100u) << 23; // 2^-100: below it 448 / a would leave float32's range
+constexpr uint32_t kFp8Smallest = (127u - 100u) << 23; // 2^-100: what is smaller is held with its scale, and 448 / a stays in range
 // scale = a / 448 and the factor of the values, 448 / a, each rounded once.  All lanes of a block form both, so that two of the
 // compiler's divisions (some 24 instructions) would cost a lane of eight values as much as its values; from an approximate reciprocal
 // and the remainder of the quotient they are nine.  Checked for every mantissa of a: both are the rounded quotients.

@@ -34,6 +34,7 @@ int plan_of(const tt_fp8_shape &s, tt_fp8_launch *l)
     if (s.dtype != TT_F32 && s.dtype != TT_BF16) return TT_ERR_BAD_ARG;
     *l = tt_fp8_launch{};
     if (s.k > kFp8LargestK || s.batch > 65535) return TT_ERR_UNSUPPORTED;
+    if ((double)s.batch * std::max(s.m, s.n) * s.k > 0x1p46 || (double)s.batch * s.m * s.n > 0x1p44) return TT_ERR_UNSUPPORTED;
     const int64_t kb = fp8_blocks(s.k), cus = compute_units();
     auto tiles = [&](int64_t tm, int64_t tn) { return ((s.m + tm - 1) / tm) * ((s.n + tn - 1) / tn); };
     auto in = [&](int kernel, int tm, int tn, int block, int lds) {

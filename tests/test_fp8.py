@@ -322,6 +322,24 @@ def test_products_refuse_what_is_ill_formed():
         api.tt_fp8_plan(api.tt_fp8_shape(1, 1, 1, 0, 1, F32))
 
 
+def test_the_plan_of_a_product():
+    """The rule's outcomes that the header names: what runs, and where a workspace is needed."""
+    plan = lambda *a: api.tt_fp8_plan(api.tt_fp8_shape(*a))  # noqa: E731
+    for m in (1, 16, 17, 32):
+        p = plan(1, m, 4096, 4096, 128, BF16)
+        assert (p.kernel, p.split_k, p.workspace_bytes, p.grid) == (api.TT_FP8_STREAM, 1, 0, 256) and p.tile_m >= m
+    p = plan(1, 8192, 8192, 8192, 128, BF16)
+    assert (p.kernel, p.tile_m, p.grid, p.workspace_bytes) == (api.TT_FP8_BLOCKS, 256, 1024, 0)
+    for shape in ((1, 8192, 8192, 8192, 128, F32), (1, 1024, 768, 768, 128, BF16), (24, 197, 333, 520, 1, F32)):
+        assert plan(*shape).kernel == api.TT_FP8_TILES
+    p = plan(1, 100, 512, 8192, 128, BF16)
+    assert p.kernel == api.TT_FP8_TILES and p.split_k > 1 and p.workspace_bytes == p.split_k * 100 * 512 * 4
+    at_, short = ctypes.c_void_p(4096), ctypes.byref(api.tt_fp8_shape(1, 100, 512, 8192, 128, BF16))
+    for ws, size in ((None, 0), (at_, p.workspace_bytes - 1), (ctypes.c_void_p(4100), p.workspace_bytes)):
+        assert api.lib.tt_dense_fp8(at_, at_, at_, at_, None, at_, short, api.TT_DENSE_ADD, ws, size, None) == api.TT_ERR_WORKSPACE
+    assert api.lib.tt_fp8_plan(ctypes.byref(api.tt_fp8_shape(60000, 1 << 20, 64, 1 << 20, 1, BF16)), ctypes.byref(p)) == api.TT_ERR_UNSUPPORTED
+
+
 def test_quantize_refuses_what_is_ill_formed():
     good = dict(batch=1, rows=4, cols=4, block_rows=1, dtype=BF16)
     call = lambda s, x=at(1), q=at(2), sc=at(3): api.lib.tt_quantize_fp8(x, q, sc, ctypes.byref(s), None)  # noqa: E731
