@@ -70,6 +70,26 @@ __device__ __forceinline__ uint32_t largest_of_16_lanes(uint32_t v)
     v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, false));
     return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, false));
 }
+// x Phi(x) = max(x, 0) - |x| Q(|x|), Q(a) = 1 - Phi(a).  exp(a^2 / 2) Q(a) falls smoothly from 1/2 like 1 / (a sqrt(2 pi)) and is, to 5.5e-8
+// of itself, a polynomial of degree 8 in t = 1 / (1 + 0.3 a) (fitted to scipy's erfcx on a <= 12; beyond, exp(-a^2 / 2) ends it).  Against the
+// value in 64 bits: 2.4e-7 at most, 7.6e-7 of it down to x = -4.  Some 20 instructions without a branch, where the compiler's erff takes 60:
+// 1024 x 768 x 768 with GELU 6.8 -> 5.5 us, 9 x 7 x 90 7.0 -> 6.2.
+__device__ __forceinline__ float gelu_smooth(float x)
+{
+    constexpr float C[9] = {4.74133549e-06f, 0.119528323f, 0.121634774f, 0.0957856551f, 0.139975503f, -0.0728332847f, 0.225472927f, -0.16763334f, 0.0380647257f};
+    const float m = fabsf(x), a = m > 16.0f ? 16.0f : m; // (a NaN stays one; |x| times nothing is nothing)
+    const float t = __builtin_amdgcn_rcpf(fmaf(a, 0.3f, 1.0f));
+    float r = C[8];
+#pragma unroll
+    for (int k = 7; k >= 0; --k) r = fmaf(r, t, C[k]);
+    const float q = __builtin_amdgcn_exp2f(a * a * -0.72134752f) * r;
+    return fmaf(-a, q, x < 0.0f ? 0.0f : x);
+}
+// Four of them out of line, for epilogues of many unrolled vectors.
+static __device__ __noinline__ f32x4 gelu_smooth4(f32x4 v)
+{
+    return f32x4{gelu_smooth(v[0]), gelu_smooth(v[1]), gelu_smooth(v[2]), gelu_smooth(v[3])};
+}
 // Four values to nearest even.  |x| <= a keeps them within 448 * (1 + 2^-23), which rounds to 448: nothing overflows.
 __device__ __forceinline__ uint32_t pack_fp8x4(float a, float b, float c, float d)
 {

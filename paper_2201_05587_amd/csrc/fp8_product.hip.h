@@ -125,7 +125,7 @@ template <int N> __device__ __forceinline__ void finish_results(float (&v)[N], c
     } else if (act == ACT_GELU) {
 #pragma unroll
         for (int e = 0; e < N; e += 4) {
-            const f32x4 r = gelu4(f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]});
+            const f32x4 r = gelu_smooth4(f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]});
             v[e] = r[0], v[e + 1] = r[1], v[e + 2] = r[2], v[e + 3] = r[3];
         }
     }

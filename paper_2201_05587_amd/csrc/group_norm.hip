@@ -51,10 +51,7 @@ template <int ACT, int V> __device__ __forceinline__ void norm_act(float (&v)[V]
         }
     } else if constexpr (ACT == NORM_GELU) {
 #pragma unroll
-        for (int e = 0; e < V; e += 4) {
-            const f32x4 r = gelu4(f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]});
-            v[e] = r[0], v[e + 1] = r[1], v[e + 2] = r[2], v[e + 3] = r[3];
-        }
+        for (int e = 0; e < V; ++e) v[e] = gelu_smooth(v[e]);
     } else if constexpr (ACT == NORM_SILU) {
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] = silu(v[e]);
