@@ -465,6 +465,7 @@ template <int DT, int V, int R, bool FP8, int ACT> __global__ void __launch_boun
 // Pixels of a thread in flight together: in the first pass and in one pass, and in the second pass where there are many
 // workgroups or few.
 constexpr int kNormBatch = 4, kNormFew = 2;
+constexpr int kNormJoined = 128; // batches that a thread of the first pass joins at most
 constexpr int norm_many(int dtype, bool fp8) { return dtype == TT_F32 && fp8 ? 4 : 8; }
 constexpr int norm_vector(int dtype, bool fp8) { return fp8 || dtype == TT_BF16 ? 8 : 4; }
 constexpr int kNormWidest = 256; // vectors of a column tile
@@ -531,23 +532,26 @@ int lay_out(const tt_norm_shape &s, bool fp8, NormLayout *lay, tt_norm_launch *l
     } else {
         // Two passes.  The first in column tiles of whole groups (of some 256 bytes, so that an image makes many workgroups and
         // still few parts) where one has room for a group; every workgroup of the second reads the statistics of all parts of its
-        // groups, so that there are at most 64 of them, and its tiles are 16 vectors wide.
+        // groups, so that there are at most 64 of them (more where a thread's float32 sums would run over more than kNormJoined
+        // batches), and its tiles are 16 vectors wide.
         const int64_t whole = (int64_t)g.wide / std::gcd(g.wide, V); // vectors of the fewest whole groups
         const int channels = (s.c + V - 1) / V; // vectors that hold any
         const bool aligned = whole <= kNormWidest || channels <= kNormWidest;
         const int first_tx = whole <= kNormWidest ? (int)std::min<int64_t>(channels, whole * ((15 + whole) / whole)) : aligned ? channels : widest;
         lay->first = tiles_of(channels, first_tx, 512, pixels);
         const int64_t others = (int64_t)s.n * lay->first.tiles;
-        set_parts(lay->first, std::min<int64_t>(64, (2 * cus + others - 1) / others), kNormBatch, pixels);
+        const int64_t longest = (int64_t)lay->first.ty * kNormBatch * kNormJoined; // pixels of a part
+        set_parts(lay->first, std::max(std::min<int64_t>(64, (2 * cus + others - 1) / others), (pixels + longest - 1) / longest), kNormBatch, pixels);
         g.stat_parts = lay->first.parts, g.stat_pixels = lay->first.part_pixels;
         g.stat_tiles = aligned ? 1 : lay->first.tiles, g.stat_width = lay->first.tx * V;
         g.div_stat_tiles = make_fastdiv((uint32_t)g.stat_tiles);
-        // The second in four workgroups a CU, with many pixels a thread at a time where it has so many.
+        // The second in at most four workgroups a CU, which run together (16 x 32 x 32 x 1280 into 8 bits 33.6 -> 32.1 us for 4.4 of
+        // them), with many pixels a thread at a time where it has so many.
         const int many = norm_many(s.dtype, fp8);
         const int threads = (int64_t)s.n * columns * pixels < 4 * cus * 512 * kNormFew ? 256 : 512;
         g.t = tiles_of(columns, std::min(columns, 16), threads, pixels);
         const int64_t besides = (int64_t)s.n * g.t.tiles;
-        set_parts(g.t, (4 * cus + besides - 1) / besides, kNormFew, pixels);
+        set_parts(g.t, 4 * cus / besides, kNormFew, pixels);
         lay->few = g.t.part_pixels < (int64_t)g.t.ty * many;
         const int64_t bytes = (int64_t)s.n * pixels * s.c * (s.dtype == TT_F32 ? 4 : 2);
         g.past = !fp8 && s.c % V == 0 && bytes >= kNormPast;
@@ -585,6 +589,7 @@ template <int DT, bool FP8> int launch(NormLayout &lay, int act, void *stream)
         g.t = lay.first;
         const int lds = g.t.ty * std::min(g.t.tx * V, g.c) * (int)sizeof(float2);
         hipLaunchKernelGGL((norm_statistics_kernel<DT, V, kNormBatch>), dim3(g.t.parts * g.t.tiles, g.n), dim3(block_of(g.t)), lds, static_cast<hipStream_t>(stream), g);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return note_hip_error((int)e, "norm_statistics_kernel launch");
     }
     lay.args.top = act == TT_ACT_RELU6 ? 6.0f : INFINITY;
     switch (act) {

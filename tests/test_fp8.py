@@ -207,7 +207,8 @@ def check_large(batch, m, n, k, b_rows, dtype, cls, seed=3):
 @pytest.mark.parametrize("b_rows", [1, 128])
 @pytest.mark.parametrize("batch,m,n,k", [(1, 2900, 3001, 640), (1, 4100, 2051, 200), (1, 2048, 4096, 128), (1, 4096, 2049, 256), (1, 2500, 3500, 384),
                                          (1, 3840, 2304, 1000), (1, 1030, 768, 4096), (1, 129, 4097, 8192), (1, 8192, 24, 1024), (40, 300, 520, 333),
-                                         (130, 256, 256, 512), (70, 130, 390, 500), (1, 1500, 1700, 5000)])
+                                         (130, 256, 256, 512), (70, 130, 390, 500), (1, 1500, 1700, 5000),
+                                         (1, 3, 20, 1 << 20), (1, 40, 70, 300_000)])
 def test_products_of_many_tiles(batch, m, n, k, b_rows, dtype):
     check_large(batch, m, n, k, b_rows, dtype, None if batch > 1 else (api.TT_DENSE_ADD, api.TT_DENSE_BIAS_RELU, api.TT_DENSE_BIAS_GELU)[(m + n) % 3])
 

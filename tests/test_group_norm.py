@@ -159,7 +159,7 @@ def test_group_norm_is_the_same_every_time_on_every_stream_and_in_a_graph():
 
 @pytest.mark.gpu
 def test_maps_beyond_32_bit_offsets():
-    n, h, w, c, groups = 3, 1300, 1300, 512, 32  # 2.6e9 elements
+    n, h, w, c, groups = 3, 1300, 1300, 512, 32  # 2.6e9 elements, in more parts than a small map's
     x = torch.empty(n, h, w, c, dtype=torch.bfloat16, device="cuda")
     for i in range(n):
         x[i].normal_()
@@ -201,6 +201,17 @@ def test_convolution_norm_and_8_bit_product_one_after_the_other():
     b2 = b2.double().numpy()
     want = np.maximum(p[0] + b2, 0)
     assert (np.abs(y.double().cpu().numpy() - want) <= 8 * 2.0 ** -13 * (size[0] + np.abs(b2)) * (1 + 2.0 ** -4) + 2.0 ** -8 * want).all()
+
+
+def test_the_plan_of_a_group_norm():
+    plan = lambda *a, fp8=False: api.tt_norm_plan(api.tt_norm_shape(*a), fp8)  # noqa: E731
+    for fp8 in (False, True):
+        assert plan(1, 3, 3, 64, 8, F32, fp8=fp8).kernel == api.TT_NORM_ONE_PASS and plan(1, 3, 3, 64, 8, F32, fp8=fp8).workspace_bytes == 0
+        p = plan(2, 64, 64, 320, 32, BF16, fp8=fp8)
+        assert p.kernel == api.TT_NORM_TWO_PASS and 1 <= p.chunks <= 64 and p.workspace_bytes == 2 * 32 * p.chunks * 8
+    # a part is never longer than float32 sums over 128 batches of four pixels a thread allow
+    p = plan(1, 1 << 15, 1 << 15, 1, 1, BF16)
+    assert p.kernel == api.TT_NORM_TWO_PASS and p.chunks * 512 * 4 * 128 >= 1 << 30 and p.workspace_bytes == p.chunks * 8
 
 
 # ---- refusals (no GPU is reached) ------------------------------------------------------------------------------------
