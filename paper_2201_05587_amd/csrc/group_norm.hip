@@ -466,6 +466,7 @@ template <int DT, int V, int R, bool FP8, int ACT> __global__ void __launch_boun
 // workgroups or few.
 constexpr int kNormBatch = 4, kNormFew = 2;
 constexpr int kNormJoined = 128; // batches that a thread of the first pass joins at most
+constexpr int norm_held(int dtype, bool fp8) { return dtype == TT_F32 && fp8 ? 8 : 16; } // of a thread in one pass, at most
 constexpr int norm_many(int dtype, bool fp8) { return dtype == TT_F32 && fp8 ? 4 : 8; }
 constexpr int norm_vector(int dtype, bool fp8) { return fp8 || dtype == TT_BF16 ? 8 : 4; }
 constexpr int kNormWidest = 256; // vectors of a column tile
@@ -496,7 +497,8 @@ int block_of(const NormTiles &t) { return (t.tx * t.ty + 63) / 64 * 64; }
 struct NormLayout {
     NormArgs args;          // without pointers; t: of the second (or only) launch
     NormTiles first;        // of the first pass
-    bool one_pass, few;     // few: kNormFew pixels a thread
+    int one_pass;           // pixels a thread holds; 0: two passes
+    bool few;               // in the second pass: kNormFew pixels a thread at a time
 };
 
 int lay_out(const tt_norm_shape &s, bool fp8, NormLayout *lay, tt_norm_launch *l)
@@ -519,12 +521,28 @@ int lay_out(const tt_norm_shape &s, bool fp8, NormLayout *lay, tt_norm_launch *l
     const int even = (columns + kNormWidest - 1) / kNormWidest; // column tiles of equal width
     const int widest = ((columns + even - 1) / even + unit - 1) / unit * unit;
 
-    // One pass: column tiles of whole groups (the fewest that are whole vectors, or all of them) whose pixels the registers of a
-    // workgroup hold.
+    // One pass: column tiles of whole groups whose pixels the registers of a workgroup hold, kNormBatch pixels a thread.  The fewest
+    // groups that are whole vectors make the most workgroups, but an image's rows in pieces of 16 bytes; where that many
+    // workgroups are not needed, tiles are wider, up to 256 bytes, and up to 128 with more pixels a thread (64 x 28 x 28 x 256 bf16 in
+    // pieces of 16 bytes 50 us, 32 bytes 25, two passes 22, 128 bytes 16; 256 x 14 x 14 x 256 50, two passes 22, here 17; 8 x 14 x 14 x 512
+    // 5.9, two passes 9.2).
+    const int held = norm_held(s.dtype, fp8);
     const int64_t group_tile = (int64_t)g.wide / std::gcd(g.wide, V * unit) * (V * unit); // channels
-    const int tile = s.c % group_tile == 0 ? (int)std::min<int64_t>(group_tile / V, columns) : columns;
-    if (tile <= kNormWidest && pixels <= (512 / tile) * (int64_t)kNormBatch) {
-        lay->one_pass = true;
+    int tile = s.c % group_tile == 0 ? (int)std::min<int64_t>(group_tile / V, columns) : columns;
+    auto fits = [&](int tx, int rows) { return tx <= kNormWidest && pixels <= (512 / tx) * (int64_t)rows; };
+    auto many_workgroups = [&](int tx) { return (int64_t)s.n * ((columns + tx - 1) / tx) >= cus; };
+    if (fits(tile, kNormBatch))
+        lay->one_pass = kNormBatch;
+    else if (fits(tile, held) && many_workgroups(tile))
+        lay->one_pass = held;
+    if (lay->one_pass) {
+        while (tile < 16 && columns % (2 * tile) == 0 && many_workgroups(2 * tile)) {
+            if (!fits(2 * tile, lay->one_pass)) {
+                if (tile >= 8 || !fits(2 * tile, held)) break;
+                lay->one_pass = held;
+            }
+            tile *= 2;
+        }
         g.t = tiles_of(columns, tile, 512, pixels);
         g.t.parts = 1, g.t.part_pixels = (int32_t)pixels;
         l->kernel = TT_NORM_ONE_PASS;
@@ -573,8 +591,11 @@ template <int DT, bool FP8, int ACT> void launch_last(const NormLayout &lay, voi
     const int stat_bytes = std::min(g.groups, width / g.wide + 2) * (int)sizeof(float2);
     const dim3 grid(g.t.parts * g.t.tiles, g.n), block(block_of(g.t));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (lay.one_pass)
-        hipLaunchKernelGGL((norm_one_pass_kernel<DT, V, kNormBatch, FP8, ACT>), grid, block, g.t.ty * width * (int)sizeof(float2) + stat_bytes, s, g);
+    const int lds = g.t.ty * width * (int)sizeof(float2) + stat_bytes;
+    if (lay.one_pass == kNormBatch)
+        hipLaunchKernelGGL((norm_one_pass_kernel<DT, V, kNormBatch, FP8, ACT>), grid, block, lds, s, g);
+    else if (lay.one_pass)
+        hipLaunchKernelGGL((norm_one_pass_kernel<DT, V, norm_held(DT, FP8), FP8, ACT>), grid, block, lds, s, g);
     else if (lay.few)
         hipLaunchKernelGGL((norm_apply_kernel<DT, V, kNormFew, FP8, ACT>), grid, block, stat_bytes, s, g);
     else

@@ -85,7 +85,8 @@ def check(n, h, w, c, groups, dtype, act, fp8=False, affine=True, eps=1e-5, offs
 SIZES = [(1, 1, 1, 1, 1), (1, 1, 1, 32, 32), (3, 1, 1, 40, 8), (1, 9, 7, 90, 9), (2, 8, 8, 128, 32), (1, 5, 3, 130, 13), (2, 16, 16, 320, 32),
          (1, 33, 17, 96, 1), (4, 7, 7, 512, 32), (1, 1, 300, 72, 3), (2, 3, 3, 2048, 32), (1, 40, 40, 64, 64), (1, 31, 29, 1000, 8), (5, 64, 48, 24, 3),
          (1, 2, 2, 10240, 4), (1, 2, 5, 5001, 3), (1, 128, 130, 16, 2), (1, 2, 1, 2048, 2048),
-         (1, 40, 30, 1000, 1000), (2, 28, 28, 128, 32), (1, 60, 60, 640, 32), (3, 50, 37, 2056, 8)]
+         (1, 40, 30, 1000, 1000), (2, 28, 28, 128, 32), (1, 60, 60, 640, 32), (3, 50, 37, 2056, 8), (17, 28, 28, 128, 32), (40, 14, 13, 64, 16),
+         (300, 3, 5, 40, 8), (70, 5, 5, 256, 2), (130, 20, 11, 24, 3), (33, 11, 40, 128, 8)]
 
 
 @pytest.mark.gpu
