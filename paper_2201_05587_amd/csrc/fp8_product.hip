@@ -8,25 +8,40 @@
 namespace tt {
 namespace {
 
-// Estimated time (us) of a launch of `tiles` workgroups over `steps` steps of the reduction, from launches of 4096 x 4096 x 4096, 8192^3
-// and m x 4096 x 4096, m = 16 .. 2048, and 1024 and 4096 x 768 x 768 (bf16, a scale in 128 rows of B; us, tiles of 64 | 128 | blocks):
-//   m = 256  13.3 | 24.3 | 47     512  17.5 | 24.8 | 47     1024  31 | 26.4 | 48     2048  62 | 58 | 50     4096  129 | 100 | 62
-//   4096 x 768 x 768  8.5 | 9.5 | 15.4     1024 x 768 x 768  4.8 | 8.4 | 14.7     8192^3  903 | 716 | 454
-// A step of a block takes 1.8 us, of 128 x 128 0.8, a workgroup on a CU at a time; of 64 x 64 a CU takes three together, a quarter of a
-// microsecond each where it has many.
-double estimate(int tile, int64_t tiles, int64_t steps, int64_t cus)
+// Estimated times (us) of a launch, fitted to launches of 1 .. 8192 rows by 64 .. 32768 columns by 64 .. 16384, 1 to 256 in a batch.
+//
+// bf16, a scale in 128 rows of B, tiles of 64 | 128 | blocks:
+//   m x 4096 x 4096, m = 256  13.3 | 24.3 | 47     512  17.5 | 24.8 | 47     1024  31 | 26.4 | 48     2048  62 | 58 | 50     4096  129 | 100 | 62
+//   4096 x 768 x 768  8.5 | 9.5 | 15.4     1024 x 768 x 768  4.8 | 8.4 | 14.7     8192^3  903 | 716 | 454     8192 x 8192 x 64  52 | 66 | 36
+// Rounds of workgroups over the CUs; of 64 x 64 a CU takes three together, and one alone is no faster than its loads.  Further:
+//   fp32 widens its operands, which costs the smaller tile more: m x 4096 x 4096, m = 512  29 | 35     1024  49 | 38     4096  179 | 144;
+//   a scale in every row of B is a product more for each output: 3012 x 2982 x 1601  31 | 41 | 32;
+//   rows of bf16 that start at odd elements are stored by halves, 64 KB of a block by one CU: 302 x 247 x 467  4.0 | 7.7 | 17.4.
+double estimate_tiles(int tile, const tt_fp8_shape &s, int64_t tiles, int64_t steps, int64_t cus)
 {
-    const double rounds = (double)((tiles + cus - 1) / cus);
+    const double full = (double)tiles / (double)cus, rounds = (double)((tiles + cus - 1) / cus), k = (double)steps;
+    const bool f32 = s.dtype == TT_F32, each = s.b_rows == 1, odd = !f32 && s.n % 2;
     switch (tile) {
-    case 64: return 3.2 + (double)steps * (tiles <= cus ? 0.28 + 0.11 * (double)tiles / (double)cus : std::max(0.2 + 0.19 * rounds, 0.25 * rounds));
-    case 128: return 4.0 + (double)steps * 0.8 * rounds;
-    default: return 6.0 + (double)steps * 1.8 * rounds;
+    case 64: return 2.6 + std::max(k * ((f32 ? 0.44 : 0.28) + 0.03 * full), rounds * (odd ? 0.8 : 0.55) + rounds * k * (f32 ? 0.36 : 0.21));
+    case 128: return 2.3 + rounds * ((odd ? 5.2 : 3.0) + k * (f32 ? 1.02 : each ? 0.72 : 0.66));
+    default: {
+        const double store = odd ? 9.0 : 0.0, step = each ? 1.6 : 1.2;
+        return full < 1.0 ? 7.3 + store + 2.0 * full + k * (step + 0.45 * full * full) : 2.3 + rounds * (7.0 + store + k * (step + 0.45));
+    }
     }
 }
 
-// Rows of A at most for the streaming kernel: it reads A once for 16 rows of B (24 x 1000 x 2048 fp32 5.2 us, in tiles 8.0; 32 x 4096 x 4096
-// 9.0 and 9.9; 64 x 4096 x 4096 13.3 and 11.1).
+// The streaming kernel reads A again for 16 rows of B, so that it leads while its workgroups are few (us, stream | tiles, their
+// reduction split where that is faster):
+//   1 x 4096 x 4096  5.6 | 8.2     12 x 4096 x 4096  6.6 | 8.5     32 x 4096 x 4096  9.1 | 9.4     24 x 1000 x 2048 fp32  5.2 | 8.0
+//   1 x 8192 x 8192  16.0 | 14.1   32 x 8192 x 8192  28 | 15.1     1 x 32768 x 1024  15.0 | 7.4    16 batches of 32 x 512 x 512  5.5 | 3.9
 constexpr int kStreamRows = 32;
+double estimate_stream(int64_t rows, int64_t workgroups, int64_t steps, int64_t cus)
+{
+    const double full = workgroups <= cus ? (double)workgroups / (double)cus : (double)((workgroups + cus - 1) / cus), k = (double)steps;
+    const double one = rows <= 16 ? 0.09 + 0.002 * (double)rows : 0.19; // a step of a workgroup that has its CU alone
+    return 2.3 + std::max(one * k, full * (rows <= 16 ? 0.75 + (0.1 + 0.0015 * (double)rows) * k : 1.3 + 0.18 * k));
+}
 
 int plan_of(const tt_fp8_shape &s, tt_fp8_launch *l)
 {
@@ -40,29 +55,28 @@ int plan_of(const tt_fp8_shape &s, tt_fp8_launch *l)
     auto in = [&](int kernel, int tm, int tn, int block, int lds) {
         l->kernel = kernel, l->tile_m = tm, l->tile_n = tn, l->split_k = 1, l->block = block, l->lds_bytes = lds;
     };
-    if (s.m <= kStreamRows) {
-        in(TT_FP8_STREAM, s.m <= 16 ? 16 : 32, 16, 512, 0);
-    } else {
+    const bool f32 = s.dtype == TT_F32;
+    in(TT_FP8_TILES, 64, 64, 256, Tiles<64, 64>::LDS);
+    double best = estimate_tiles(64, s, tiles(64, 64) * s.batch, kb, cus);
+    // fp32 with a scale per row of B holds too much for the larger tile's registers
+    if (!f32 || s.b_rows > 1)
+        if (const double us = estimate_tiles(128, s, tiles(128, 128) * s.batch, kb, cus); us < best) best = us, in(TT_FP8_TILES, 128, 128, 256, Tiles<128, 128>::LDS);
+    if (!f32)
+        if (const double us = estimate_tiles(256, s, tiles(256, 256) * s.batch, kb, cus); us < best) best = us, in(TT_FP8_BLOCKS, 256, 256, Fp8Block::THREADS, Fp8Block::LDS);
+    if (s.m <= kStreamRows)
+        if (const double us = estimate_stream(s.m, tiles(kStreamRows, 16) * s.batch, kb, cus); us < best) best = us, in(TT_FP8_STREAM, s.m <= 16 ? 16 : 32, 16, 512, 0);
+    // Few tiles and a long reduction: splits of it, whose sums a second launch adds, from a workspace written and read.
+    // 100 x 512 x 8192: 21 us, 4 splits 11.1, 8 10.6, 16 13.5; 300 x 1000 x 1000 7.8 us, 2 splits 8.9; 200 x 8192 x 4096 17.9 us, 8 splits 38.
+    int splits = 1;
+    for (int n = 2; n <= 16 && n * 2 <= kb; n *= 2) {
+        const double sums = 2.5 + 0.35 * n + (double)n * s.batch * s.m * s.n * 4 / 2.5e6;
+        if (const double us = estimate_tiles(64, s, tiles(64, 64) * s.batch * n, (kb + n - 1) / n, cus) + sums; us < best) best = us, splits = n;
+    }
+    if (splits > 1) {
         in(TT_FP8_TILES, 64, 64, 256, Tiles<64, 64>::LDS);
-        double best = estimate(64, tiles(64, 64) * s.batch, kb, cus);
-        // fp32 with a scale per row of B holds too much for the larger tile's registers
-        if (s.dtype == TT_BF16 || s.b_rows > 1)
-            if (const double us = estimate(128, tiles(128, 128) * s.batch, kb, cus); us < best) best = us, in(TT_FP8_TILES, 128, 128, 256, Tiles<128, 128>::LDS);
-        if (s.dtype == TT_BF16)
-            if (const double us = estimate(256, tiles(256, 256) * s.batch, kb, cus); us < best) best = us, in(TT_FP8_BLOCKS, 256, 256, Fp8Block::THREADS, Fp8Block::LDS);
-        // Few tiles and a long reduction: splits of it, whose sums a second launch adds (3.5 us, and a third of one for every split).
-        // 100 x 512 x 8192: 21 us, 4 splits 11.1, 8 10.6, 16 13.5; 300 x 1000 x 1000 7.8 us, 2 splits 8.9.
-        int splits = 1;
-        for (int n = 2; n <= 16 && n * 2 <= kb; n *= 2) {
-            const double us = estimate(64, tiles(64, 64) * s.batch * n, (kb + n - 1) / n, cus) + 3.5 + 0.35 * n;
-            if (us < best) best = us, splits = n;
-        }
-        if (splits > 1) {
-            in(TT_FP8_TILES, 64, 64, 256, Tiles<64, 64>::LDS);
-            const int64_t steps = (kb + splits - 1) / splits;
-            l->split_k = (int32_t)((kb + steps - 1) / steps);
-            l->workspace_bytes = (int64_t)l->split_k * s.batch * s.m * s.n * 4;
-        }
+        const int64_t steps = (kb + splits - 1) / splits;
+        l->split_k = (int32_t)((kb + steps - 1) / steps);
+        l->workspace_bytes = (int64_t)l->split_k * s.batch * s.m * s.n * 4;
     }
     const int64_t grid = tiles(l->tile_m, l->tile_n);
     if (grid * l->block > INT32_MAX) return TT_ERR_UNSUPPORTED;
