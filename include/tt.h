@@ -331,8 +331,8 @@ int tt_dwconv(const void *x, const void *w, const void *bias, void *y, const tt_
  *
  * tt_quantize_fp8: x [batch, rows, cols] of `dtype` into that form.  For every block a = max(max |x|, 2^-100), scale = a / 448 rounded
  * to float32, and value = x * 448 / a rounded once, to the nearest e4m3, ties to even.  A block that holds an infinity or a NaN has
- * that as its scale, and everything computed from the block is NaN.  TT_ERR_UNSUPPORTED: 2^26 rows or more in all, or more than 2^22
- * columns.
+ * that as its scale, and everything computed from the block is NaN.  TT_ERR_UNSUPPORTED: 2^26 rows or 2^23 blocks of 128 rows
+ * or more in all, or more than 2^22 columns.
  */
 #define TT_FP8_BLOCK 128
 typedef struct tt_quant_shape {

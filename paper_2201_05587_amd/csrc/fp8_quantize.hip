@@ -143,6 +143,8 @@ int check_quant_shape(const tt_quant_shape &s)
 {
     if (s.batch < 1 || s.rows < 1 || s.cols < 1 || (s.block_rows != 1 && s.block_rows != kFp8Block)) return TT_ERR_BAD_ARG;
     if (s.dtype != TT_F32 && s.dtype != TT_BF16) return TT_ERR_BAD_ARG;
+    const int64_t squares = (int64_t)s.batch * (((int64_t)s.rows + kFp8Block - 1) / kFp8Block); // of a column block, 512 threads each
+    if (s.block_rows == kFp8Block && squares >= 1ll << 23) return TT_ERR_UNSUPPORTED;
     return (int64_t)s.batch * s.rows >= kFp8LargestRows || s.cols > kFp8LargestK ? TT_ERR_UNSUPPORTED : TT_OK;
 }
 

@@ -351,6 +351,8 @@ def test_quantize_refuses_what_is_ill_formed():
         assert call(s, **change) == api.TT_ERR_BAD_ARG, change
     assert call(api.tt_quant_shape(1, 1, (1 << 22) + 1, 1, BF16)) == api.TT_ERR_UNSUPPORTED
     assert call(api.tt_quant_shape(1 << 13, 1 << 13, 1, 1, BF16)) == api.TT_ERR_UNSUPPORTED
+    # a workgroup of 512 threads for every block of rows: 2^32 threads
+    assert call(api.tt_quant_shape(1 << 23, 1, 1, 128, BF16)) == api.TT_ERR_UNSUPPORTED
 
 
 def status(call):
