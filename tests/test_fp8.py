@@ -213,6 +213,30 @@ def test_products_of_many_tiles(batch, m, n, k, b_rows, dtype):
     check_large(batch, m, n, k, b_rows, dtype, None if batch > 1 else (api.TT_DENSE_ADD, api.TT_DENSE_BIAS_RELU, api.TT_DENSE_BIAS_GELU)[(m + n) % 3])
 
 
+# (tile, splits of the reduction, shape): every launch form with rows of B and N that end inside a tile, even and odd
+LAUNCHES = [(16, False, (1, 12, 1003, 2000, 1, BF16)), (32, False, (2, 31, 333, 900, 128, F32)),
+            (64, False, (40, 7, 531, 140, 1, BF16)), (64, False, (64, 30, 299, 200, 128, F32)), (64, False, (1, 3, 20001, 200, 128, BF16)),
+            (64, True, (1, 17, 1023, 8192, 128, BF16)), (64, True, (3, 29, 100, 9000, 1, F32)), (64, True, (2, 40, 100, 8100, 1, BF16)),
+            (128, False, (1, 4464, 649, 1896, 1, BF16)), (128, False, (3, 3507, 265, 1192, 128, BF16)), (128, False, (1, 3508, 908, 262, 128, BF16)),
+            (128, False, (50, 490, 70, 727, 1, BF16)), (128, False, (3, 322, 3133, 132, 128, F32)),
+            (256, False, (1, 3488, 4487, 274, 1, BF16)), (256, False, (1, 4115, 3809, 144, 128, BF16)), (256, False, (50, 244, 1093, 399, 1, BF16)),
+            (256, False, (3, 1412, 2168, 102, 128, BF16)), (256, False, (1, 2700, 3901, 1700, 128, BF16))]
+
+
+def test_the_launch_forms_are_the_ones_meant():
+    for tile, split, shape in LAUNCHES:
+        p = api.tt_fp8_plan(api.tt_fp8_shape(*shape))
+        assert (p.tile_m, p.split_k > 1) == (tile, split), shape
+        assert p.kernel == {16: api.TT_FP8_STREAM, 32: api.TT_FP8_STREAM, 256: api.TT_FP8_BLOCKS}.get(tile, api.TT_FP8_TILES)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [shape for _, _, shape in LAUNCHES])
+def test_every_launch_form(shape):
+    batch = shape[0]
+    check_large(*shape, None if batch > 1 else (api.TT_DENSE_ADD, api.TT_DENSE_BIAS_RELU, api.TT_DENSE_BIAS_GELU)[sum(shape) % 3])
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("m", [1, 40, 300, 1100])
