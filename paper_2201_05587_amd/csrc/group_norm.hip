@@ -58,19 +58,51 @@ template <int ACT, int V> __device__ __forceinline__ void norm_act(float (&v)[V]
     }
 }
 
-// V consecutive channels: whole 16-byte items at any element's address, and the row's last ones in part.
+// V consecutive channels, `count` of them (at least one) in their row of c: whole 16-byte items at any element's address.  An item that is
+// cut off by the row's end is loaded as the row's last 16 bytes, and settle() moves its channels to the front once they are wanted: loads
+// of single elements under their conditions wait for one another (48 x 17 x 95 x 330 bf16 59 -> 43 us, as long as 336 channels take).  What
+// lies behind `count` is anything.
 template <int DT, int V> struct Channels {
-    static constexpr int W = V / ElemOf<DT>::CH;
+    static constexpr int CH = ElemOf<DT>::CH, W = V / CH;
     u32x4 raw[W];
-    __device__ __forceinline__ void load(const void *p, int64_t at, int count)
+    __device__ __forceinline__ void load_whole(const void *p, int64_t at)
     {
-        if (count >= V) {
 #pragma unroll
-            for (int w = 0; w < W; ++w) load16(raw[w], static_cast<const typename ElemOf<DT>::type *>(p) + at + w * ElemOf<DT>::CH);
-        } else {
+        for (int w = 0; w < W; ++w) load16(raw[w], static_cast<const typename ElemOf<DT>::type *>(p) + at + w * CH);
+    }
+    __device__ __forceinline__ void load(const void *p, int64_t at, int count, int c)
+    {
+        using E = typename ElemOf<DT>::type;
+        const E *const from = static_cast<const E *>(p) + at;
+        if (c >= CH) { // (an item with no channel at all, too: it is in the row)
 #pragma unroll
-            for (int w = 0; w < W; ++w)
-                raw[w] = count > w * ElemOf<DT>::CH ? load_piece<DT>(p, at + w * ElemOf<DT>::CH, count - w * ElemOf<DT>::CH) : u32x4{0u, 0u, 0u, 0u};
+            for (int w = 0; w < W; ++w) load16(raw[w], from + w * CH - max(0, (w + 1) * CH - count));
+        } else { // the row is shorter than an item
+#pragma unroll
+            for (int w = 0; w < W; ++w) raw[w] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int e = 0; e < CH - 1; ++e) {
+                const E x = from[min(e, count - 1)];
+                if constexpr (DT == TT_F32)
+                    raw[0][e] = __float_as_uint(x);
+                else
+                    raw[0][e / 2] |= (uint32_t)x << (16 * (e % 2));
+            }
+        }
+    }
+    __device__ __forceinline__ void settle(int count, int c)
+    {
+        if (count >= V || c < CH) return;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const int by = (w + 1) * CH - count; // elements
+            u32x4 &r = raw[w];
+            if (by <= 0 || by >= CH) continue;
+            const int dwords = DT == TT_F32 ? by : by / 2;
+            if (dwords & 2) r[0] = r[2], r[1] = r[3];
+            if (dwords & 1) r[0] = r[1], r[1] = r[2], r[2] = r[3];
+            if (DT == TT_BF16 && (by & 1))
+                r[0] = r[0] >> 16 | r[1] << 16, r[1] = r[1] >> 16 | r[2] << 16, r[2] = r[2] >> 16 | r[3] << 16, r[3] >>= 16;
         }
     }
     __device__ __forceinline__ float operator[](int e) const { return element_of<DT>(raw[e / ElemOf<DT>::CH], e % ElemOf<DT>::CH); }
@@ -189,12 +221,23 @@ struct NormPlace {
 // R pixels of a thread, all loads in flight together (pixels past the end: the last one again).
 template <int DT, int V, int R> struct Pixels {
     Channels<DT, V> x[R];
-    __device__ __forceinline__ void request(const NormArgs &g, const NormPlace &at, int first)
+    template <bool WHOLE> __device__ __forceinline__ void request(const NormArgs &g, const NormPlace &at, int first)
     {
-        if (at.count > 0) {
+        if (at.count <= 0) return;
+        auto from = [&](int i) { return at.base + (int64_t)min(first + i * g.t.ty, at.end - 1) * g.c; };
+        if constexpr (WHOLE) {
 #pragma unroll
-            for (int i = 0; i < R; ++i) x[i].load(g.x, at.base + (int64_t)min(first + i * g.t.ty, at.end - 1) * g.c, at.count);
+            for (int i = 0; i < R; ++i) x[i].load_whole(g.x, from(i));
+        } else {
+#pragma unroll
+            for (int i = 0; i < R; ++i) x[i].load(g.x, from(i), at.count, g.c);
         }
+    }
+    template <bool WHOLE> __device__ __forceinline__ void settle(const NormArgs &g, const NormPlace &at)
+    {
+        if constexpr (WHOLE) return;
+#pragma unroll
+        for (int i = 0; i < R; ++i) x[i].settle(at.count, g.c);
     }
 };
 
@@ -301,7 +344,7 @@ __device__ __forceinline__ void join_groups(const NormArgs &g, const NormPlace &
 }
 
 // First pass: the statistics of a part of an image.  The next batch is requested before the present one is summed.
-template <int DT, int V, int R> __global__ void __launch_bounds__(512) norm_statistics_kernel(const NormArgs g)
+template <int DT, int V, int R, bool WHOLE> __global__ void __launch_bounds__(512) norm_statistics_kernel(const NormArgs g)
 {
     extern __shared__ float2 joined[]; // [row of threads][channel of the tile]
     NormPlace at;
@@ -311,11 +354,12 @@ template <int DT, int V, int R> __global__ void __launch_bounds__(512) norm_stat
         const int step = g.t.ty * R;
         Pixels<DT, V, R> now, next;
         int first = at.begin + at.ty;
-        if (first < at.end) now.request(g, at, first);
+        if (first < at.end) now.template request<WHOLE>(g, at, first);
         while (first < at.end) {
             const int rows = min(R, (at.end - first + g.t.ty - 1) / g.t.ty);
             const bool more = first + step < at.end;
-            if (more) next.request(g, at, first + step);
+            if (more) next.template request<WHOLE>(g, at, first + step);
+            now.template settle<WHOLE>(g, at);
             mine.join(now, rows);
             if (more) now = next;
             first += step;
@@ -409,47 +453,51 @@ template <int DT, int V, int R, bool FP8, int ACT> struct Apply {
         }
     }
 };
-template <int DT, int V> __device__ __forceinline__ void request_weights(const NormArgs &g, const NormPlace &at, Channels<DT, V> &gamma, Channels<DT, V> &beta)
+template <bool WHOLE, int DT, int V> __device__ __forceinline__ void request_weights(const NormArgs &g, const NormPlace &at, Channels<DT, V> &gamma, Channels<DT, V> &beta)
 {
-    if (at.count > 0 && g.gamma) gamma.load(g.gamma, at.channel, at.count);
-    if (at.count > 0 && g.beta) beta.load(g.beta, at.channel, at.count);
+    if (at.count <= 0) return;
+    if (g.gamma) WHOLE ? gamma.load_whole(g.gamma, at.channel) : gamma.load(g.gamma, at.channel, at.count, g.c);
+    if (g.beta) WHOLE ? beta.load_whole(g.beta, at.channel) : beta.load(g.beta, at.channel, at.count, g.c);
 }
 
 // Second pass.  The first batch of pixels is requested before the statistics are joined.
-template <int DT, int V, int R, bool FP8, int ACT> __global__ void __launch_bounds__(512) norm_apply_kernel(const NormArgs g)
+template <int DT, int V, int R, bool FP8, int ACT, bool WHOLE> __global__ void __launch_bounds__(512) norm_apply_kernel(const NormArgs g)
 {
     extern __shared__ float2 stat[]; // of the tile's groups
     NormPlace at;
     at.init<V>(g);
     Pixels<DT, V, R> p;
     int first = at.begin + at.ty;
-    p.request(g, at, first);
+    p.template request<WHOLE>(g, at, first);
     Channels<DT, V> gamma, beta;
-    request_weights(g, at, gamma, beta);
+    request_weights<WHOLE>(g, at, gamma, beta);
     join_statistics(g, at, stat);
     if (FP8 ? at.ty >= g.t.ty : at.count <= 0) return;
     Apply<DT, V, R, FP8, ACT> apply;
+    if constexpr (!WHOLE) gamma.settle(at.count, g.c), beta.settle(at.count, g.c);
     apply.init(g, at, stat, gamma, beta);
     for (;;) {
+        p.template settle<WHOLE>(g, at);
         apply.run(g, at, p, first);
         first += g.t.ty * R;
         if (first >= at.end) break;
-        p.request(g, at, first);
+        p.template request<WHOLE>(g, at, first);
     }
 }
 
 // Both in one: an image's pixels of whole groups in the registers of a workgroup.
-template <int DT, int V, int R, bool FP8, int ACT> __global__ void __launch_bounds__(512) norm_one_pass_kernel(const NormArgs g)
+template <int DT, int V, int R, bool FP8, int ACT, bool WHOLE> __global__ void __launch_bounds__(512) norm_one_pass_kernel(const NormArgs g)
 {
     extern __shared__ float2 joined[]; // [row of threads][channel of the tile], behind them mean and 1 / sqrt(var + eps) of the groups
     NormPlace at;
     at.init<V>(g);
     float2 *const stat = joined + g.t.ty * (at.tile_end - at.tile_begin);
     Pixels<DT, V, R> p;
-    p.request(g, at, at.ty);
+    p.template request<WHOLE>(g, at, at.ty);
     Channels<DT, V> gamma, beta;
-    request_weights(g, at, gamma, beta);
+    request_weights<WHOLE>(g, at, gamma, beta);
     ChannelStatistics<DT, V, R> mine;
+    p.template settle<WHOLE>(g, at);
     if (at.count > 0) mine.join(p, min(R, (g.pixels - at.ty + g.t.ty - 1) / g.t.ty));
     join_groups<V>(g, at, mine, joined, [&](int k, float mean, float squares) {
         stat[k] = float2{mean, 1.0f / sqrtf(squares * (float)g.each + g.eps)};
@@ -457,6 +505,7 @@ template <int DT, int V, int R, bool FP8, int ACT> __global__ void __launch_boun
     __syncthreads();
     if (FP8 ? at.ty >= g.t.ty : at.count <= 0) return;
     Apply<DT, V, R, FP8, ACT> apply;
+    if constexpr (!WHOLE) gamma.settle(at.count, g.c), beta.settle(at.count, g.c);
     apply.init(g, at, stat, gamma, beta);
     apply.run(g, at, p, at.ty);
 }
@@ -518,8 +567,6 @@ int lay_out(const tt_norm_shape &s, bool fp8, NormLayout *lay, tt_norm_launch *l
     const int V = norm_vector(s.dtype, fp8), unit = fp8 ? 16 : 1;
     g.div_wide_vectors = make_fastdiv((uint32_t)std::max(1, g.wide / V));
     const int columns = (int32_t)(fp8 ? fp8_blocks(s.c) * 16 : (s.c + V - 1) / V);
-    const int even = (columns + kNormWidest - 1) / kNormWidest; // column tiles of equal width
-    const int widest = ((columns + even - 1) / even + unit - 1) / unit * unit;
 
     // One pass: column tiles of whole groups whose pixels the registers of a workgroup hold, kNormBatch pixels a thread.  The fewest
     // groups that are whole vectors make the most workgroups, but an image's rows in pieces of 16 bytes; where that many
@@ -552,16 +599,18 @@ int lay_out(const tt_norm_shape &s, bool fp8, NormLayout *lay, tt_norm_launch *l
         // still few parts) where one has room for a group; every workgroup of the second reads the statistics of all parts of its
         // groups, so that there are at most 64 of them (more where a thread's float32 sums would run over more than kNormJoined
         // batches), and its tiles are 16 vectors wide.
-        const int64_t whole = (int64_t)g.wide / std::gcd(g.wide, V); // vectors of the fewest whole groups
-        const int channels = (s.c + V - 1) / V; // vectors that hold any
+        const int SV = norm_vector(s.dtype, false); // (vectors of eight fp32 channels would hold too many registers: 129)
+        const int64_t whole = (int64_t)g.wide / std::gcd(g.wide, SV); // vectors of the fewest whole groups
+        const int channels = (s.c + SV - 1) / SV; // vectors that hold any
+        const int even = (channels + kNormWidest - 1) / kNormWidest; // column tiles of equal width
         const bool aligned = whole <= kNormWidest || channels <= kNormWidest;
-        const int first_tx = whole <= kNormWidest ? (int)std::min<int64_t>(channels, whole * ((15 + whole) / whole)) : aligned ? channels : widest;
+        const int first_tx = whole <= kNormWidest ? (int)std::min<int64_t>(channels, whole * ((15 + whole) / whole)) : aligned ? channels : (channels + even - 1) / even;
         lay->first = tiles_of(channels, first_tx, 512, pixels);
         const int64_t others = (int64_t)s.n * lay->first.tiles;
         const int64_t longest = (int64_t)lay->first.ty * kNormBatch * kNormJoined; // pixels of a part
         set_parts(lay->first, std::max(std::min<int64_t>(64, (2 * cus + others - 1) / others), (pixels + longest - 1) / longest), kNormBatch, pixels);
         g.stat_parts = lay->first.parts, g.stat_pixels = lay->first.part_pixels;
-        g.stat_tiles = aligned ? 1 : lay->first.tiles, g.stat_width = lay->first.tx * V;
+        g.stat_tiles = aligned ? 1 : lay->first.tiles, g.stat_width = lay->first.tx * SV;
         g.div_stat_tiles = make_fastdiv((uint32_t)g.stat_tiles);
         // The second in at most four workgroups a CU, which run together (16 x 32 x 32 x 1280 into 8 bits 33.6 -> 32.1 us for 4.4 of
         // them), with many pixels a thread at a time where it has so many.
@@ -583,7 +632,8 @@ int lay_out(const tt_norm_shape &s, bool fp8, NormLayout *lay, tt_norm_launch *l
     return TT_OK;
 }
 
-template <int DT, bool FP8, int ACT> void launch_last(const NormLayout &lay, void *stream)
+// (WHOLE: rows of c are whole vectors)
+template <int DT, bool FP8, int ACT, bool WHOLE> void launch_last(const NormLayout &lay, void *stream)
 {
     constexpr int V = norm_vector(DT, FP8);
     const NormArgs &g = lay.args;
@@ -593,34 +643,43 @@ template <int DT, bool FP8, int ACT> void launch_last(const NormLayout &lay, voi
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int lds = g.t.ty * width * (int)sizeof(float2) + stat_bytes;
     if (lay.one_pass == kNormBatch)
-        hipLaunchKernelGGL((norm_one_pass_kernel<DT, V, kNormBatch, FP8, ACT>), grid, block, lds, s, g);
+        hipLaunchKernelGGL((norm_one_pass_kernel<DT, V, kNormBatch, FP8, ACT, WHOLE>), grid, block, lds, s, g);
     else if (lay.one_pass)
-        hipLaunchKernelGGL((norm_one_pass_kernel<DT, V, norm_held(DT, FP8), FP8, ACT>), grid, block, lds, s, g);
+        hipLaunchKernelGGL((norm_one_pass_kernel<DT, V, norm_held(DT, FP8), FP8, ACT, WHOLE>), grid, block, lds, s, g);
     else if (lay.few)
-        hipLaunchKernelGGL((norm_apply_kernel<DT, V, kNormFew, FP8, ACT>), grid, block, stat_bytes, s, g);
+        hipLaunchKernelGGL((norm_apply_kernel<DT, V, kNormFew, FP8, ACT, WHOLE>), grid, block, stat_bytes, s, g);
     else
-        hipLaunchKernelGGL((norm_apply_kernel<DT, V, norm_many(DT, FP8), FP8, ACT>), grid, block, stat_bytes, s, g);
+        hipLaunchKernelGGL((norm_apply_kernel<DT, V, norm_many(DT, FP8), FP8, ACT, WHOLE>), grid, block, stat_bytes, s, g);
 }
 
-template <int DT, bool FP8> int launch(NormLayout &lay, int act, void *stream)
+template <int DT, bool FP8, bool WHOLE> int launch(NormLayout &lay, int act, void *stream)
 {
-    constexpr int V = norm_vector(DT, FP8);
     if (!lay.one_pass) {
+        constexpr int V = norm_vector(DT, false);
         NormArgs g = lay.args;
         g.t = lay.first;
+        g.div_wide_vectors = make_fastdiv((uint32_t)std::max(1, g.wide / V));
         const int lds = g.t.ty * std::min(g.t.tx * V, g.c) * (int)sizeof(float2);
-        hipLaunchKernelGGL((norm_statistics_kernel<DT, V, kNormBatch>), dim3(g.t.parts * g.t.tiles, g.n), dim3(block_of(g.t)), lds, static_cast<hipStream_t>(stream), g);
+        // (fp32 rows of whole vectors of eight are rows of whole vectors of four)
+        hipLaunchKernelGGL((norm_statistics_kernel<DT, V, kNormBatch, WHOLE>), dim3(g.t.parts * g.t.tiles, g.n), dim3(block_of(g.t)), lds, static_cast<hipStream_t>(stream), g);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return note_hip_error((int)e, "norm_statistics_kernel launch");
     }
     lay.args.top = act == TT_ACT_RELU6 ? 6.0f : INFINITY;
     switch (act) {
-    case TT_ACT_NONE: launch_last<DT, FP8, NORM_NONE>(lay, stream); break;
-    case TT_ACT_GELU: launch_last<DT, FP8, NORM_GELU>(lay, stream); break;
-    case TT_ACT_SILU: launch_last<DT, FP8, NORM_SILU>(lay, stream); break;
-    default: launch_last<DT, FP8, NORM_CLAMP>(lay, stream); break;
+    case TT_ACT_NONE: launch_last<DT, FP8, NORM_NONE, WHOLE>(lay, stream); break;
+    case TT_ACT_GELU: launch_last<DT, FP8, NORM_GELU, WHOLE>(lay, stream); break;
+    case TT_ACT_SILU: launch_last<DT, FP8, NORM_SILU, WHOLE>(lay, stream); break;
+    default: launch_last<DT, FP8, NORM_CLAMP, WHOLE>(lay, stream); break;
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? TT_OK : note_hip_error((int)e, "group norm launch");
+}
+
+template <bool FP8> int launch(NormLayout &lay, int dtype, int act, void *stream)
+{
+    const bool whole = lay.args.c % norm_vector(dtype, FP8) == 0;
+    if (dtype == TT_F32) return whole ? launch<TT_F32, FP8, true>(lay, act, stream) : launch<TT_F32, FP8, false>(lay, act, stream);
+    return whole ? launch<TT_BF16, FP8, true>(lay, act, stream) : launch<TT_BF16, FP8, false>(lay, act, stream);
 }
 
 int run(const void *x, const void *gamma, const void *beta, void *y, float *scale, const tt_norm_shape *shape, int act, float eps,
@@ -636,8 +695,7 @@ int run(const void *x, const void *gamma, const void *beta, void *y, float *scal
     if (l.workspace_bytes > 0 && (!ws || !aligned16(ws) || (int64_t)ws_bytes < l.workspace_bytes)) return TT_ERR_WORKSPACE;
     NormArgs &g = lay.args;
     g.x = x, g.gamma = gamma, g.beta = beta, g.y = y, g.scale = scale, g.ws = static_cast<float2 *>(ws), g.eps = eps;
-    if (fp8) return shape->dtype == TT_F32 ? launch<TT_F32, true>(lay, act, stream) : launch<TT_BF16, true>(lay, act, stream);
-    return shape->dtype == TT_F32 ? launch<TT_F32, false>(lay, act, stream) : launch<TT_BF16, false>(lay, act, stream);
+    return fp8 ? launch<true>(lay, shape->dtype, act, stream) : launch<false>(lay, shape->dtype, act, stream);
 }
 
 } // namespace

@@ -118,6 +118,33 @@ def test_means_far_from_zero_and_groups_without_variance(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("c,groups", [(1, 1), (2, 1), (3, 3), (5, 1), (6, 3), (7, 7), (9, 3), (11, 1), (12, 3), (13, 13), (14, 2), (15, 5), (17, 1), (23, 1),
+                                      (129, 3), (131, 1), (258, 6), (1003, 17)])
+def test_rows_that_end_inside_an_item(c, groups, fp8):
+    """In one pass and in two; rows shorter than an item of 16 bytes, and every length behind one."""
+    for dtype in (F32, BF16):
+        for n, h, w in ((1, 1, 1), (2, 5, 4), (2, 41, 37), (300, 3, 3)):
+            check(n, h, w, c, groups, dtype, ACTS[(h + c) % 5], fp8, affine=h != 5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("h", [3, 64])
+@pytest.mark.parametrize("c,groups", [(15, 3), (6, 2), (90, 9)])
+def test_what_is_not_finite_stays_in_its_group_where_rows_end_inside_an_item(c, groups, h, dtype):
+    x, gamma, beta = make(1, 3, h, h, c, dtype)
+    wide = c // groups
+    x[0, 0, 0, wide - 1], x[1, 1, 2, c - 1], x[2, 0, 1, wide] = float("nan"), float("nan"), float("inf")
+    y = api.tt_group_norm_act(x.cuda(), gamma.cuda(), beta.cuda(), api.tt_norm_shape(3, h, h, c, groups, dtype), api.TT_ACT_NONE, 1e-5).cpu()
+    lost = torch.isnan(y).view(3, h * h, groups, wide)
+    want = torch.zeros(3, groups, dtype=torch.bool)
+    want[0, 0] = want[1, groups - 1] = want[2, 1] = True
+    assert torch.equal(lost.any(dim=3).any(dim=1), want)
+    assert bool(lost[1, :, groups - 1].all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("h", [3, 64])
 def test_what_is_not_finite_stays_in_its_image_and_group(h):
     x, gamma, beta = make(1, 3, h, h, 64, F32)
