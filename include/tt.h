@@ -349,6 +349,7 @@ int tt_quantize_fp8(const void *x, void *q, float *scale, const tt_quant_shape *
  * which every e4m3 value fits exactly.  bf16 results are summed by the 8-bit matrix cores, twice as fast; those add products in
  * runs of eight and cut each off 13 bits below the largest of its run, so that a result is off by less than 7 * 2^-13 of the sum
  * of its absolute products (rows of normal values: 2^-16 of the result, where a bf16 result's own rounding is 2^-8).
+ * Two scales of tt_quantize_fp8 may be so small or so large that float32 does not hold their product, where it holds the result.
  *   tt_dense_fp8         classes TT_DENSE_ADD, TT_DENSE_BIAS_RELU, TT_DENSE_BIAS_GELU; batch 1; bias may be NULL
  *   tt_batch_matmul_fp8  no bias, no activation; any batch
  * They stand outside the schedule records: the library chooses the launch from the shape, tt_fp8_plan says which, and how large a

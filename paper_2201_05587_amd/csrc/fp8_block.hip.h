@@ -105,26 +105,33 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
     };
-    // the scales of quadrant (h, k) of step t
+    // the scales of quadrant (h, k) of step t: of A (times that of B, where it is one), and of B's rows
     float sa[4], sb[B_ROWS == 1 ? 8 : 1];
+    struct Scales {
+        float a[4], b[B_ROWS == 1 ? 8 : 1];
+    };
     auto read_scales = [&](int h, int k, int t) {
         const float *const from = reinterpret_cast<const float *>(smem + 2 * S::SLICE + (t % S::RING) * S::SCALES);
+        Scales s;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sa[i] = from[h * 128 + a_row + i * 16];
-        if constexpr (B_ROWS == 1) {
+        for (int e = 0; e < (B_ROWS == 1 ? 8 : 1); ++e) s.b[e] = from[256 + k * 128 + (B_ROWS == 1 ? wn * 32 + lane_g * 8 + e : 0)];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sb[e] = from[256 + k * 128 + wn * 32 + lane_g * 8 + e];
-        } else {
-            sb[0] = from[256 + k * 128];
+        for (int i = 0; i < 4; ++i) s.a[i] = from[h * 128 + a_row + i * 16];
+        return s;
+    };
+    auto take_scales = [&](const Scales &s) {
+        __builtin_amdgcn_sched_barrier(0); // (waits for them behind the FMAs of finish)
+        const float raised = s.b[0] * kRaised;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sa[i] *= sb[0];
-        }
+        for (int i = 0; i < 4; ++i) sa[i] = B_ROWS == 1 ? s.a[i] : s.a[i] * raised;
+#pragma unroll
+        for (int e = 0; e < (B_ROWS == 1 ? 8 : 1); ++e) sb[e] = s.b[e];
     };
     f32x4 part[8]; // products of the matrix instructions of a quadrant, 2 i + j
     auto accumulate = [&](f32x4 (&c)[4][2], int x) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            c[x / 2][x % 2][e] = fmaf(part[x][e], B_ROWS == 1 ? sa[x / 2] * sb[(x % 2 * 4 + e) % (B_ROWS == 1 ? 8 : 1)] : sa[x / 2], c[x / 2][x % 2][e]);
+            c[x / 2][x % 2][e] = add_near<B_ROWS>(part[x][e], sa[x / 2], sb[(x % 2 * 4 + e) % (B_ROWS == 1 ? 8 : 1)], sa[x / 2], c[x / 2][x % 2][e]);
     };
     constexpr int LAG = 3; // matrix instructions issued before the first one's products are used
     auto multiply = [&](f32x4 (&c)[4][2], const P::Operand (&b)[2]) {
@@ -156,8 +163,9 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
         // phase 0
         read_a(0, buffer);
         request_b(1, t + 1, buffer ^ 1);
+        const Scales s00 = read_scales(0, 0, t);
         if (t > 0) finish(acc[1][0]);
-        read_scales(0, 0, t);
+        take_scales(s00);
         wait_loads_outstanding<9>(); // B1 of this step has landed (the other team reads it a turn later)
         swap_teams();
         multiply(acc[0][0], b0);
@@ -165,8 +173,9 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
         // phase 1
         read_b(b1, 1, buffer);
         request_a(1, t + 1, buffer ^ 1);
+        const Scales s01 = read_scales(0, 1, t);
         finish(acc[0][0]);
-        read_scales(0, 1, t);
+        take_scales(s01);
         wait_loads_outstanding<9>(); // A1 of this step
         swap_teams();
         multiply(acc[0][1], b1);
@@ -174,8 +183,9 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
         // phase 2
         read_a(1, buffer);
         request_a(0, t + 2, buffer);
+        const Scales s11 = read_scales(1, 1, t);
         finish(acc[0][1]);
-        read_scales(1, 1, t);
+        take_scales(s11);
         wait_loads_outstanding<6>(); // A0, B0 and scales of the next step
         swap_teams();
         multiply(acc[1][1], b1);
@@ -184,8 +194,9 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
         read_b(b1, 0, buffer ^ 1);
         request_b(0, t + 2, buffer);
         request_scales(t + 2);
+        const Scales s10 = read_scales(1, 0, t);
         finish(acc[1][1]);
-        read_scales(1, 0, t);
+        take_scales(s10);
         swap_teams();
         multiply(acc[1][0], b0);
         swap_teams();
@@ -197,6 +208,18 @@ template <int B_ROWS> __global__ void __launch_bounds__(512) product_block_kerne
     finish(acc[1][0]);
     if (team == 0) swap_teams(); // team 1 is one turn behind
     wait_loads_outstanding<0>(); // the requests past the end: nothing may still write the LDS when the workgroup ends
+    float none = 0.0f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            f32x4 &sum = acc[h][x / 8][x / 2 % 4][x % 2];
+            note_not_finite(none, sum);
+            if constexpr (B_ROWS > 1) sum *= 1.0f / kRaised;
+        }
+    if (__builtin_expect(wave_sums_again(none), 0))
+        return store_with_any_scales<TT_BF16, B_ROWS>(g, 8, 2, 0, kb, [&](int i) { return m0 + i / 4 * 128 + a_row + i % 4 * 16; },
+                                                      [&](int j) { return n0 + j * 128 + b_row; }, [&](int j) { return n0 + j * 128 + wn * 32 + lane_g * 8; });
 
 #pragma unroll
     for (int k = 0; k < 2; ++k) {

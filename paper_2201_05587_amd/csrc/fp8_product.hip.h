@@ -76,6 +76,55 @@ template <> struct BlockProduct<TT_F32> {
     }
 };
 
+// A block's sum p counts p * sa * sb.  p is 0 or between 2^-18 and 2^25 (128 products of e4m3 values), and scales go from 2^-109 to 2^119 (a / 448,
+// a from 2^-100 on), so that p * sa * sb may be an ordinary float32 number where a part of it is not: two scales of 2^-70 leave
+// ten bits of their product, and two of 2^70 an infinity, which makes a NaN of a sum of 0.
+//   rows of B that share a scale: sa * sb is formed once for all sums of a row of A, times 2^92, which makes the smallest (2^-218, zeros beside
+//   zeros) a normal number, and the sums are taken back by 2^-92 at the end: the same bits;
+//   a scale for each row of B: (p * sa) * sb, as many instructions as p * (sa * sb), where p * sa is 2^-127 at least.
+// What overflows that way (results from 2^36 on, or scales beyond any use) leaves a sum that is not finite.  A wave that has one computes its sums
+// again, from memory, the smaller scale first where sa * sb or p * sa is no ordinary number: p * smaller overflows only where both are
+// above 2^100 and the result is infinite too.  (Where every wave does, 4096^3 takes 1.4 ms for 63 us; with both ways in the loop the
+// accumulators do not fit the registers, and looking at every scale there costs a tenth.)
+constexpr float kRaised = 0x1p92f;
+// x * 0 added up: a NaN once one of the values is not finite
+__device__ __forceinline__ void note_not_finite(float &none, f32x4 v)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) none = fmaf(v[e], 0.0f, none);
+}
+__device__ __forceinline__ bool wave_sums_again(float none) { return __builtin_amdgcn_ballot_w64(none != none) != 0; }
+template <int B_ROWS> __device__ __forceinline__ float add_near(float p, float sa, float sb, float both, float sum) // both: sa * sb, raised or not
+{
+    return B_ROWS > 1 ? fmaf(p, both, sum) : fmaf(p * sa, sb, sum);
+}
+template <int B_ROWS> __device__ __forceinline__ float add_any(float p, float sa, float sb, float sum)
+{
+    const float both = sa * sb, first = B_ROWS > 1 ? both : p * sa;
+    const bool swap = fabsf(sa) > fabsf(sb);
+    const bool near = B_ROWS > 1 ? __builtin_isnormal(first) : __builtin_isfinite(first);
+    return near ? add_near<B_ROWS>(p, sa, sb, both, sum) : fmaf(p * (swap ? sb : sa), swap ? sa : sb, sum);
+}
+// The sums of one lane over steps begin, begin + by ..: a, b: its row's piece of step 0; a_scale: of its row, b_scale: of four rows of B.
+template <int DT, int B_ROWS>
+__device__ __forceinline__ f32x4 sums_of_any_scales(const ProductArgs &g, const uint8_t *a, const uint8_t *b, const float *a_scale, const float *b_scale,
+                                                    const int (&b_row)[4], int begin, int end, int by)
+{
+    using P = BlockProduct<DT>;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int t = begin; t < end; t += by) {
+        Fragment x, y;
+        load16(x.lo, a + t * kFp8Block), load16(x.hi, a + t * kFp8Block + 64);
+        load16(y.lo, b + t * kFp8Block), load16(y.hi, b + t * kFp8Block + 64);
+        const f32x4 p = P::run(P::operand(P::hold(y)), P::operand(P::hold(x)));
+        const float sa = a_scale[(int64_t)t * g.M];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = add_any<B_ROWS>(p[e], sa, b_scale[(int64_t)t * g.b_scale_row + b_row[e]], sum[e]);
+    }
+    return sum;
+}
+
 // Position of a row's 16-byte pieces in the LDS: piece c of row r lies at c ^ swizzle(r).  A fragment's 16 lanes read one piece of
 // 16 rows, which the swizzle spreads over all banks (256 bytes, two rows).
 //   rows of A: r, r + 1, ... r + 15;   rows of B: 8 (i / 4) + i % 4 (+ 4), i = 0 .. 15, so that the matrix cores leave eight
@@ -129,6 +178,43 @@ template <int N> __device__ __forceinline__ void finish_results(float (&v)[N], c
             v[e] = r[0], v[e + 1] = r[1], v[e + 2] = r[2], v[e + 3] = r[3];
         }
     }
+}
+
+// Pieces of 16 rows of A by 32 of B, stored: a_row(i), b_row(j): the rows that the lane multiplies, of B the first of two, 4 apart; n(j): the first of
+// the eight outputs that it then holds.
+template <int DT, int B_ROWS, class RowOfA, class RowOfB, class N>
+__device__ __forceinline__ void store_with_any_scales(const ProductArgs &g, int pieces_of_a, int pieces_of_b, int begin, int end, RowOfA &&a_row, RowOfB &&b_row, N &&n_of)
+{
+    const int64_t batch = blockIdx.y, kp = (int64_t)g.kb * kFp8Block;
+    const int piece = (int)(threadIdx.x & 63) / 16 * 16;
+#pragma unroll 1
+    for (int i = 0; i < pieces_of_a; ++i)
+#pragma unroll 1
+        for (int j = 0; j < pieces_of_b; ++j) {
+            const int m = a_row(i), n = n_of(j), m_in = min(m, g.M - 1); // rows past a matrix read its last row; what they give is not stored
+            float v[8];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                int scale_row[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) scale_row[e] = min(n + half * 4 + e, g.N - 1) / B_ROWS;
+                const f32x4 sum = sums_of_any_scales<DT, B_ROWS>(
+                    g, g.a + (batch * g.M + m_in) * kp + piece, g.b + (batch * g.N + min(b_row(j) + half * 4, g.N - 1)) * kp + piece,
+                    g.a_scale + batch * g.kb * g.M + m_in, g.b_scale + batch * g.kb * g.b_scale_row, scale_row, begin, end, 1);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[half * 4 + e] = sum[e];
+            }
+            if (m >= g.M || n >= g.N) continue;
+            const int64_t at = (batch * g.M + m) * g.N + n;
+            if (g.splits > 1)
+                store_eight<TT_F32>(g.ws + (int64_t)blockIdx.z * g.batch * g.M * g.N, at, v, g.N - n);
+            else {
+                float bias[8] = {};
+                if (g.bias) load_eight<DT>(bias, g.bias, n, g.N - n);
+                finish_results<8>(v, bias, g.act);
+                store_eight<DT>(g.out, at, v, g.N - n);
+            }
+        }
 }
 
 // Tile `wg` of tiles_m x tiles_n: a contiguous run of tiles per XCD, walked in bands of `band` tile rows, so that the tiles an XCD
@@ -194,10 +280,21 @@ template <int DT, int MS> __global__ void __launch_bounds__(512) product_stream_
 #pragma unroll
             for (int i = 0; i < MS; ++i) {
                 const f32x4 p = P::run(bx, P::operand(P::hold(y[u][i])));
+                const float raised = sa[u][i] * kRaised;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[i][e] = fmaf(p[e], sa[u][i] * sb[u][e], sum[i][e]);
+                for (int e = 0; e < 4; ++e) sum[i][e] = fmaf(p[e], raised * sb[u][e], sum[i][e]);
             }
         }
+    }
+    float none = 0.0f;
+#pragma unroll
+    for (int i = 0; i < MS; ++i) {
+        note_not_finite(none, sum[i]);
+        sum[i] *= 1.0f / kRaised; // (the scales are multiplied with each other first, whatever b_rows)
+    }
+    if (__builtin_expect(wave_sums_again(none), 0)) {
+#pragma unroll
+        for (int i = 0; i < MS; ++i) sum[i] = sums_of_any_scales<DT, kFp8Block>(g, a[i], b, a_scale + row[i], b_scale, b_row, wave, g.kb, S::WAVES);
     }
 #pragma unroll
     for (int i = 0; i < MS; ++i) sums[wave][i][lane] = sum[i];
@@ -310,8 +407,9 @@ template <int DT, int TM, int TN, int B_ROWS> __global__ void __launch_bounds__(
         constexpr int COUNT = S::MI * S::NJ, LAG = COUNT < 8 ? 2 : 3; // matrix instructions issued before the first one's products are used
         const unsigned char *const from = smem + (t % S::RING) * S::STAGE + b_scale_at;
         if constexpr (B_ROWS > 1) {
+            const float raised = sb[0] * kRaised;
 #pragma unroll
-            for (int i = 0; i < S::MI; ++i) sa[i] *= sb[0];
+            for (int i = 0; i < S::MI; ++i) sa[i] *= raised;
         }
         f32x4 part[COUNT], sb_next = sb;
         auto accumulate = [&](int x) {
@@ -321,7 +419,7 @@ template <int DT, int TM, int TN, int B_ROWS> __global__ void __launch_bounds__(
                 if (j + 1 < S::NJ) sb_next = *reinterpret_cast<const f32x4 *>(from + 4 * ((j + 1) / 2 * 32 + (j + 1) % 2 * 4));
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[x][e], B_ROWS == 1 ? sa[i] * sb[e] : sa[i], acc[i][j][e]);
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = add_near<B_ROWS>(part[x][e], sa[i], sb[e], sa[i], acc[i][j][e]);
             asm volatile("" : "+v"(acc[i][j])); // (keeps the FMAs here, between the matrix instructions)
         };
         if constexpr (DT == TT_BF16) {
@@ -382,6 +480,17 @@ template <int DT, int TM, int TN, int B_ROWS> __global__ void __launch_bounds__(
             multiply(now, sa, sb, t);
         }
     wait_loads_outstanding<0>(); // the requests past the end: nothing may still write the LDS when the workgroup ends
+    float none = 0.0f;
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) {
+            note_not_finite(none, acc[i][j]);
+            if constexpr (B_ROWS > 1) acc[i][j] *= 1.0f / kRaised;
+        }
+    if (__builtin_expect(wave_sums_again(none), 0))
+        return store_with_any_scales<DT, B_ROWS>(g, S::MI, S::NJ / 2, begin, end, [&](int i) { return m0 + a_row + i * 16; },
+                                                 [&](int j) { return n0 + b_row + j * 32; }, [&](int j) { return n0 + wn * S::WN + lane_g * 8 + j * 32; });
 #pragma unroll
     for (int jj = 0; jj < S::NJ / 2; ++jj) {
         const int n = n0 + wn * S::WN + jj * 32 + lane_g * 8;

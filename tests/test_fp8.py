@@ -237,6 +237,92 @@ def test_every_launch_form(shape):
     check_large(*shape, None if batch > 1 else (api.TT_DENSE_ADD, api.TT_DENSE_BIAS_RELU, api.TT_DENSE_BIAS_GELU)[sum(shape) % 3])
 
 
+# ---- scales whose product leaves float32's range ---------------------------------------------------------------------
+# (every launch form with a scale per row of B and per 128)
+FAR_SHAPES = [shape for _, _, shape in LAUNCHES] + [(1, 3, 40, 300, 1, F32), (1, 3, 40, 300, 128, F32), (2, 100, 200, 300, 1, F32), (1, 100, 200, 300, 128, F32)]
+
+
+def blocks_on_gpu(x, group, dtype=F32):
+    return api.tt_quantize_fp8(x, api.tt_quant_shape(*x.shape, group, dtype))
+
+
+def in_64_bits(q, s, group):
+    kb = q.shape[-1] // 128
+    wide = s.double().repeat_interleave(group, dim=2)[:, :, :q.shape[1]].transpose(1, 2).unsqueeze(3)
+    return (q.double().view(*q.shape[:2], kb, 128) * wide).flatten(2)
+
+
+def far_tolerance(ref, size, kb, dtype):
+    """The tolerance of a product, and half a step of the smallest float32 number for every addition (bf16: of the result)."""
+    tol = (128 + 2 * kb + 4) * 2.0 ** -23 * size + (kb + 2) * 2.0 ** -150
+    return tol if dtype == F32 else (tol + 7 * 2.0 ** -13 * size) * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 2.0 ** -134
+
+
+def check_far(a, b, shape):
+    batch, m, n, k, b_rows, dtype = shape
+    (qa, sa), (qb, sb) = blocks_on_gpu(a, 1), blocks_on_gpu(b, b_rows)
+    y = torch.full((batch, m, n), float("nan"), dtype=api.torch_dtype(dtype), device="cuda")
+    api.tt_batch_matmul_fp8(qa, sa, qb, sb, api.tt_fp8_shape(*shape), c=y)
+    for i in range(batch):
+        x, w = in_64_bits(qa[i:i + 1], sa[i:i + 1], 1)[0], in_64_bits(qb[i:i + 1], sb[i:i + 1], b_rows)[0]
+        ref, size = x @ w.t().contiguous(), x.abs() @ w.abs().t().contiguous()
+        err, tol = (y[i].double() - ref).abs(), far_tolerance(ref, size, -(-k // 128), dtype)
+        assert bool((err <= tol).all()), (i, int((~(err <= tol)).sum()), torch.nonzero(~(err <= tol))[:4].tolist())
+    return y
+
+
+def normal_rows(gen, batch, rows, cols, exponents):
+    """Normal values times a power of two for every row."""
+    return torch.randn((batch, rows, cols), generator=gen, device="cuda") * torch.exp2(exponents(batch, rows).float()).unsqueeze(2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", FAR_SHAPES)
+def test_products_of_two_small_scales(shape):
+    """Scales of 2^-71 to 2^-63: their products have between 17 and 5 bits in float32, the results all of them."""
+    batch, m, n, k, b_rows, _ = shape
+    gen = torch.Generator(device="cuda").manual_seed(m + n)
+    exponents = lambda *s: torch.randint(-64, -57, s, generator=gen, device="cuda")  # noqa: E731
+    check_far(normal_rows(gen, batch, m, k, exponents), normal_rows(gen, batch, n, k, exponents), shape)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", FAR_SHAPES)
+def test_products_of_two_large_scales_over_a_sum_of_zero(shape):
+    """Column blocks of ordinary, far and far opposite scales; where both are large, one operand has the even columns and the other
+    the odd ones, so that the block counts nothing."""
+    batch, m, n, k, b_rows, _ = shape
+    gen = torch.Generator(device="cuda").manual_seed(m + n)
+    even = torch.arange(k, device="cuda") % 2 == 0
+    block = torch.arange(k, device="cuda") // 128 % 6
+    of_a, of_b = (torch.tensor(e, device="cuda", dtype=torch.float64)[block] for e in ((0, 75, 100, -70, 118, -100), (0, 75, -100, -70, 118, 98)))
+    apart = (block == 1) | (block == 4)
+    a = torch.randn((batch, m, k), generator=gen, device="cuda", dtype=torch.float64).clamp(-4, 4) * torch.exp2(of_a) * ~(apart & even)
+    b = torch.randn((batch, n, k), generator=gen, device="cuda", dtype=torch.float64).clamp(-4, 4) * torch.exp2(of_b) * ~(apart & ~even)
+    check_far(a.float(), b.float(), shape)
+    a, b = a * (block == 4), b * (block == 4)
+    if k > 4 * 128:
+        assert not bool(check_far(a.float(), b.float(), shape).any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", FAR_SHAPES)
+def test_far_scales_leave_the_other_rows_as_they_are(shape):
+    """Bit for bit: a row of zeros beside small weights (2^-109 times 2^-22), and a row near the largest float32 number."""
+    batch, m, n, k, b_rows, dtype = shape
+    gen = torch.Generator(device="cuda").manual_seed(m + n)
+    a, b = (torch.randn((batch, r, k), generator=gen, device="cuda") for r in (m, n))
+    (qb, sb), s = blocks_on_gpu(b * 2.0 ** -15, b_rows), api.tt_fp8_shape(*shape)
+    want = api.tt_batch_matmul_fp8(*blocks_on_gpu(a, 1), qb, sb, s)
+    for factor in (0.0, 2.0 ** 120):
+        other = a.clone()
+        other[:, m // 2] *= factor
+        got = api.tt_batch_matmul_fp8(*blocks_on_gpu(other, 1), qb, sb, s)
+        rest = torch.arange(m, device="cuda") != m // 2
+        assert torch.equal(got[:, rest], want[:, rest])
+        assert bool(torch.isfinite(got[:, m // 2]).all()) and (factor != 0 or not bool(got[:, m // 2].any()))
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("m", [1, 40, 300, 1100])
