@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "fp8_block.hip.h"
 
@@ -52,35 +53,34 @@ int plan_of(const tt_fp8_shape &s, tt_fp8_launch *l)
     if ((double)s.batch * std::max(s.m, s.n) * s.k > 0x1p46 || (double)s.batch * s.m * s.n > 0x1p44) return TT_ERR_UNSUPPORTED;
     const int64_t kb = fp8_blocks(s.k), cus = compute_units();
     auto tiles = [&](int64_t tm, int64_t tn) { return ((s.m + tm - 1) / tm) * ((s.n + tn - 1) / tn); };
-    auto in = [&](int kernel, int tm, int tn, int block, int lds) {
-        l->kernel = kernel, l->tile_m = tm, l->tile_n = tn, l->split_k = 1, l->block = block, l->lds_bytes = lds;
-    };
     const bool f32 = s.dtype == TT_F32;
-    in(TT_FP8_TILES, 64, 64, 256, Tiles<64, 64>::LDS);
-    double best = estimate_tiles(64, s, tiles(64, 64) * s.batch, kb, cus);
+    double best = INFINITY;
+    // The fastest of those whose workgroups a launch can have.
+    auto consider = [&](double us, int kernel, int tm, int tn, int block, int lds) {
+        if (us >= best || tiles(tm, tn) * block > INT32_MAX) return false;
+        best = us;
+        l->kernel = kernel, l->tile_m = tm, l->tile_n = tn, l->split_k = 1, l->block = block, l->lds_bytes = lds;
+        return true;
+    };
+    consider(estimate_tiles(64, s, tiles(64, 64) * s.batch, kb, cus), TT_FP8_TILES, 64, 64, 256, Tiles<64, 64>::LDS);
     // fp32 with a scale per row of B holds too much for the larger tile's registers
-    if (!f32 || s.b_rows > 1)
-        if (const double us = estimate_tiles(128, s, tiles(128, 128) * s.batch, kb, cus); us < best) best = us, in(TT_FP8_TILES, 128, 128, 256, Tiles<128, 128>::LDS);
-    if (!f32)
-        if (const double us = estimate_tiles(256, s, tiles(256, 256) * s.batch, kb, cus); us < best) best = us, in(TT_FP8_BLOCKS, 256, 256, Fp8Block::THREADS, Fp8Block::LDS);
-    if (s.m <= kStreamRows)
-        if (const double us = estimate_stream(s.m, tiles(kStreamRows, 16) * s.batch, kb, cus); us < best) best = us, in(TT_FP8_STREAM, s.m <= 16 ? 16 : 32, 16, 512, 0);
+    if (!f32 || s.b_rows > 1) consider(estimate_tiles(128, s, tiles(128, 128) * s.batch, kb, cus), TT_FP8_TILES, 128, 128, 256, Tiles<128, 128>::LDS);
+    if (!f32) consider(estimate_tiles(256, s, tiles(256, 256) * s.batch, kb, cus), TT_FP8_BLOCKS, 256, 256, Fp8Block::THREADS, Fp8Block::LDS);
+    if (s.m <= kStreamRows) consider(estimate_stream(s.m, tiles(kStreamRows, 16) * s.batch, kb, cus), TT_FP8_STREAM, s.m <= 16 ? 16 : 32, 16, 512, 0);
     // Few tiles and a long reduction: splits of it, whose sums a second launch adds, from a workspace written and read.
     // 100 x 512 x 8192: 21 us, 4 splits 11.1, 8 10.6, 16 13.5; 300 x 1000 x 1000 7.8 us, 2 splits 8.9; 200 x 8192 x 4096 17.9 us, 8 splits 38.
     int splits = 1;
     for (int n = 2; n <= 16 && n * 2 <= kb; n *= 2) {
         const double sums = 2.5 + 0.35 * n + (double)n * s.batch * s.m * s.n * 4 / 2.5e6;
-        if (const double us = estimate_tiles(64, s, tiles(64, 64) * s.batch * n, (kb + n - 1) / n, cus) + sums; us < best) best = us, splits = n;
+        if (consider(estimate_tiles(64, s, tiles(64, 64) * s.batch * n, (kb + n - 1) / n, cus) + sums, TT_FP8_TILES, 64, 64, 256, Tiles<64, 64>::LDS)) splits = n;
     }
+    if (best == INFINITY) return TT_ERR_UNSUPPORTED;
     if (splits > 1) {
-        in(TT_FP8_TILES, 64, 64, 256, Tiles<64, 64>::LDS);
         const int64_t steps = (kb + splits - 1) / splits;
         l->split_k = (int32_t)((kb + steps - 1) / steps);
         l->workspace_bytes = (int64_t)l->split_k * s.batch * s.m * s.n * 4;
     }
-    const int64_t grid = tiles(l->tile_m, l->tile_n);
-    if (grid * l->block > INT32_MAX) return TT_ERR_UNSUPPORTED;
-    l->grid = (int32_t)grid;
+    l->grid = (int32_t)tiles(l->tile_m, l->tile_n);
     return TT_OK;
 }
 

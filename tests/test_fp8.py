@@ -451,6 +451,16 @@ def test_the_plan_of_a_product():
     assert api.lib.tt_fp8_plan(ctypes.byref(api.tt_fp8_shape(60000, 1 << 20, 64, 1 << 20, 1, BF16)), ctypes.byref(p)) == api.TT_ERR_UNSUPPORTED
 
 
+def test_a_product_is_refused_only_where_no_launch_has_so_many_workgroups():
+    largest = 2 ** 31 - 1  # threads of a grid
+    for shape, tile in (((1, 1 << 20, 1 << 15, 64, 128, F32), 128), ((1, 1, 1 << 29, 64, 128, BF16), 128), ((1, 16, 1 << 29, 64, 1, BF16), 128),
+                        ((1, 40, (1 << 29) + 77, 300, 128, F32), 128)):
+        p = api.tt_fp8_plan(api.tt_fp8_shape(*shape))
+        assert p.tile_m == tile and p.grid * p.block <= largest, shape
+    for shape in ((1, 1, 1 << 30, 64, 128, BF16), (1, 1 << 20, 1 << 15, 64, 1, F32)):  # (fp32 with a scale per row of b has the small tile only)
+        assert api.lib.tt_fp8_plan(ctypes.byref(api.tt_fp8_shape(*shape)), ctypes.byref(api.tt_fp8_launch())) == api.TT_ERR_UNSUPPORTED
+
+
 def test_quantize_refuses_what_is_ill_formed():
     good = dict(batch=1, rows=4, cols=4, block_rows=1, dtype=BF16)
     call = lambda s, x=at(1), q=at(2), sc=at(3): api.lib.tt_quantize_fp8(x, q, sc, ctypes.byref(s), None)  # noqa: E731
