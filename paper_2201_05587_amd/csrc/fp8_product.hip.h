@@ -112,7 +112,7 @@ __device__ __forceinline__ f32x4 sums_of_any_scales(const ProductArgs &g, const 
 {
     using P = BlockProduct<DT>;
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
+#pragma unroll 1
     for (int t = begin; t < end; t += by) {
         Fragment x, y;
         load16(x.lo, a + t * kFp8Block), load16(x.hi, a + t * kFp8Block + 64);
