@@ -216,7 +216,8 @@ PyObject *py_dwconv(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 // ---- matrices held in 8 bits, group norm ----------------------------------------------------------------
 // Unlike the records' operators these know the type and size of every argument, so a tensor is taken only if it is of that
-// type, as large as the shape says, dense, and on the current device.  (What is no plain tensor is the caller's own memory.)
+// type, as large as the shape says, dense, and on the current device, whatever its class.  (What is no tensor is the caller's own
+// memory.)
 
 PyObject *quant_shape_type, *fp8_shape_type, *norm_shape_type;
 
@@ -224,23 +225,25 @@ class Checked {
 public:
     void *address(PyObject *o, at::ScalarType type, int64_t numel)
     {
-        if (!THPVariable_CheckExact(o)) return address_of(o);
+        if (!is_tensor(o)) return address_of(o);
         const at::Tensor &t = THPVariable_Unpack(o);
         good_ = good_ && t.scalar_type() == type && t.numel() == numel && t.is_contiguous() && on_device(t);
-        return good_ ? t.data_ptr() : nullptr;
+        return good_ ? address_of(o) : nullptr;
     }
     // A workspace is memory of any type; `bytes`: how many there are.
     void *workspace(PyObject *o, size_t *bytes)
     {
         *bytes = o == Py_None ? 0 : bytes_of(o);
-        if (!THPVariable_CheckExact(o)) return address_of(o);
+        if (!is_tensor(o)) return address_of(o);
         const at::Tensor &t = THPVariable_Unpack(o);
         good_ = good_ && t.is_contiguous() && on_device(t);
-        return good_ ? t.data_ptr() : nullptr;
+        return good_ ? address_of(o) : nullptr;
     }
     bool good() const { return good_; }
 
 private:
+    // (a call that asks Python about an argument's class is left to those that are neither)
+    static bool is_tensor(PyObject *o) { return THPVariable_CheckExact(o) || (o != Py_None && THPVariable_Check(o)); }
     static bool on_device(const at::Tensor &t) { return t.is_cuda() && t.device().index() == c10::hip::current_device(); }
     bool good_ = true;
 };

@@ -495,6 +495,31 @@ def test_the_binding_refuses_tensors_that_are_not_what_the_shape_says():
     assert status(lambda: api.tt_dense_fp8(x, x, x, x, None, api.tt_fp8_shape(1, 4, 4, -4, 1, F32), api.TT_DENSE_ADD)) == api.TT_ERR_BAD_ARG
 
 
+class Labelled(torch.Tensor):
+    """A tensor of a class of its own."""
+
+
+def test_the_binding_looks_at_tensors_of_other_classes_too():
+    x = torch.zeros(4, 4).as_subclass(Labelled)  # on the CPU: its address is none for the GPU
+    assert status(lambda: api.tt_quantize_fp8(x, api.tt_quant_shape(1, 4, 4, 1, F32))) == api.TT_ERR_BAD_ARG
+    assert status(lambda: api.tt_dense_fp8(x, x, x, x, None, api.tt_fp8_shape(1, 4, 4, 4, 1, F32), api.TT_DENSE_ADD)) == api.TT_ERR_BAD_ARG
+    assert status(lambda: api.tt_group_norm_act(x, None, None, api.tt_norm_shape(1, 1, 4, 4, 1, F32))) == api.TT_ERR_BAD_ARG
+
+
+@pytest.mark.gpu
+def test_tensors_of_other_classes_on_the_gpu():
+    x = torch.randn(4, 200, device="cuda")
+    shape = api.tt_quant_shape(1, 4, 200, 1, F32)
+    want, got = api.tt_quantize_fp8(x, shape), api.tt_quantize_fp8(x.as_subclass(Labelled), shape)
+    assert torch.equal(want[0].float(), got[0].float()) and torch.equal(want[1], got[1])
+    for wrong in (x[:2], x.bfloat16(), x.cpu(), torch.randn(200, 4, device="cuda").t()):
+        assert status(lambda: api.tt_quantize_fp8(wrong.as_subclass(Labelled), shape)) == api.TT_ERR_BAD_ARG
+    ws = torch.zeros(1 << 20, dtype=torch.uint8).as_subclass(Labelled)  # a workspace on the CPU
+    w = api.tt_quantize_fp8(torch.randn(512, 8192, device="cuda"), api.tt_quant_shape(1, 512, 8192, 128, F32))
+    a = api.tt_quantize_fp8(torch.randn(100, 8192, device="cuda"), api.tt_quant_shape(1, 100, 8192, 1, F32))
+    assert status(lambda: api.tt_dense_fp8(*a, *w, None, api.tt_fp8_shape(1, 100, 512, 8192, 128, BF16), api.TT_DENSE_ADD, ws=ws)) == api.TT_ERR_BAD_ARG
+
+
 @pytest.mark.gpu
 def test_the_binding_refuses_other_types_sizes_and_strides_on_the_gpu():
     bad = api.TT_ERR_BAD_ARG
