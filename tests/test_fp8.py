@@ -10,6 +10,7 @@ Tolerances of products, S = the sum of the absolute values of an output's produc
   GELU's slope is at most 1.13 and its own evaluation is off by 2^-20 of the value.
 """
 import ctypes
+import math
 
 import numpy as np
 import pytest
@@ -235,6 +236,47 @@ def test_the_launch_forms_are_the_ones_meant():
 def test_every_launch_form(shape):
     batch = shape[0]
     check_large(*shape, None if batch > 1 else (api.TT_DENSE_ADD, api.TT_DENSE_BIAS_RELU, api.TT_DENSE_BIAS_GELU)[sum(shape) % 3])
+
+
+# ---- GELU over its range ---------------------------------------------------------------------------------------------
+# x Q(|x|), Q = exp(-x^2 / 2) times a smooth factor: the factor, the exponential's own rounding and the last ones are off by some 13
+# roundings of 2^-24 (the polynomial 5.5e-8, nine steps of it at most twice its value, a reciprocal, an exponential), less than
+# 2^-20; the exponent, a product of three numbers rounded twice and once more with its constant, by 2.6 * 2^-24 of x^2 / 2, which is
+# what a rounding of x itself would change.  Below 2^-126 the exponential is 0.
+def gelu_sweep(dtype):
+    """(values, their GELU in 64 bits, tolerance)"""
+    v = np.concatenate([np.linspace(-20, 20, 2001), np.linspace(-150, 150, 300), [1e-30, -1e-30, 1e30, -1e30, 3e38, -3e38, -0.0]]).astype(np.float32)
+    v = torch.from_numpy(v).to(api.torch_dtype(dtype))
+    x = v.double().numpy()
+    tail = np.array([0.5 * abs(t) * math.erfc(abs(t) / math.sqrt(2.0)) for t in x])  # |x| Q(|x|)
+    y = np.maximum(x, 0.0) - tail
+    tol = 2.0 ** -20 * np.abs(y) + 1.3 * 2.0 ** -24 * np.minimum(x * x, 1e6) * tail + 2.0 ** -126
+    return v, y, tol if dtype == F32 else tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(y) + 2.0 ** -134
+
+
+GELU_SHAPES = [(1, 128, 1, F32), (1, 128, 128, BF16), (30, 300, 128, F32), (70, 200, 1, F32), (90, 8192, 1, F32), (2700, 2048, 128, F32), (1300, 2048, 1, BF16),
+               (4000, 500, 128, BF16)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,k,b_rows,dtype", GELU_SHAPES)
+def test_gelu_over_its_range(m, k, b_rows, dtype):
+    """As the bias of a product of zeros."""
+    v, y, tol = gelu_sweep(dtype)
+    n, kb = len(v), -(-k // 128)
+    zeros = lambda rows: torch.zeros(rows, kb * 128, device="cuda").to(E4M3)  # noqa: E731
+    ones = lambda rows: torch.ones(kb, rows, device="cuda")  # noqa: E731
+    got = api.tt_dense_fp8(zeros(m), ones(m), zeros(n), ones(-(-n // b_rows)), v.cuda(), api.tt_fp8_shape(1, m, n, k, b_rows, dtype), api.TT_DENSE_BIAS_GELU)
+    assert bool((got == got[:1]).all())
+    bad = ~(np.abs(got[0].double().cpu().numpy() - y) <= tol)
+    assert not bad.any(), (int(bad.sum()), v[bad][:8])
+
+
+def test_the_gelu_sweep_meets_every_kernel():
+    n = len(gelu_sweep(F32)[0])
+    plans = [api.tt_fp8_plan(api.tt_fp8_shape(1, m, n, k, b_rows, dtype)) for m, k, b_rows, dtype in GELU_SHAPES]
+    assert {(p.kernel, p.tile_m, p.split_k > 1) for p in plans} == {(api.TT_FP8_STREAM, 16, False), (api.TT_FP8_STREAM, 32, False), (api.TT_FP8_TILES, 64, False),
+                                                                   (api.TT_FP8_TILES, 64, True), (api.TT_FP8_TILES, 128, False), (api.TT_FP8_BLOCKS, 256, False)}
 
 
 # ---- scales whose product leaves float32's range ---------------------------------------------------------------------

@@ -7,6 +7,7 @@ The activations' slopes are at most 1.13, and their own evaluation is off by 2^-
 themselves; the 8-bit ones 2^-4 of themselves, 2^-10 of the scale, and the scale's error once more.
 """
 import ctypes
+import math
 
 import numpy as np
 import pytest
@@ -115,6 +116,33 @@ def test_means_far_from_zero_and_groups_without_variance(dtype):
     ones, zeros = torch.ones(32).to(x.dtype), torch.zeros(32).to(x.dtype)
     y = api.tt_group_norm_act(x.cuda(), ones.cuda(), zeros.cuda(), api.tt_norm_shape(2, 10, 10, 32, 4, dtype), api.TT_ACT_NONE, 1e-5)
     assert not bool(y.any())  # exactly the mean
+
+
+# An activation's own error.  GELU: test_fp8.py's bound.  SiLU, v / (1 + exp(-v)): a product, a sum, an exponential and a reciprocal of
+# less than 2^-20 together, and the exponent, rounded with its constant, by 1.5 * 2^-24 of |v|; a reciprocal below 2^-126 is 0.
+@pytest.mark.gpu
+@pytest.mark.parametrize("h", [2, 8])  # in one pass, and in two
+@pytest.mark.parametrize("act", [api.TT_ACT_GELU, api.TT_ACT_SILU])
+def test_activations_over_their_range(act, h):
+    """As the shift of values times zero."""
+    v = np.concatenate([np.linspace(-20, 20, 2000), np.linspace(-150, 150, 993), [1e-30, -1e-30, 1e30, -1e30, 3e38, -3e38, -0.0]]).astype(np.float32)
+    x, c = v.astype(np.float64), 1000
+    if act == api.TT_ACT_GELU:
+        tail = np.array([0.5 * abs(t) * math.erfc(abs(t) / math.sqrt(2.0)) for t in x])
+        y = np.maximum(x, 0.0) - tail
+        tol = 2.0 ** -20 * np.abs(y) + 1.3 * 2.0 ** -24 * np.minimum(x * x, 1e6) * tail + 2.0 ** -126
+    else:
+        with np.errstate(over="ignore"):
+            y = x / (1.0 + np.exp(-x))
+        tol = np.abs(y) * (2.0 ** -20 + 1.5 * 2.0 ** -24 * np.minimum(np.abs(x), 1e3)) + np.minimum(np.abs(x), 1e3) * 2.0 ** -126
+    shape = api.tt_norm_shape(1, h, h, c, 1, F32)
+    assert api.tt_norm_plan(shape).kernel == (api.TT_NORM_ONE_PASS if h == 2 else api.TT_NORM_TWO_PASS)
+    some = make(1, 1, h, h, c, F32)[0].cuda()
+    for i in range(0, len(v), c):
+        got = api.tt_group_norm_act(some, torch.zeros(c, device="cuda"), torch.from_numpy(v[i:i + c]).cuda(), shape, act).view(h * h, c)
+        assert bool((got == got[:1]).all())
+        bad = ~(np.abs(got[0].double().cpu().numpy() - y[i:i + c]) <= tol[i:i + c])
+        assert not bad.any(), (int(bad.sum()), v[i:i + c][bad][:8])
 
 
 @pytest.mark.gpu
