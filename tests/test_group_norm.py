@@ -118,6 +118,41 @@ def test_means_far_from_zero_and_groups_without_variance(dtype):
     assert not bool(y.any())  # exactly the mean
 
 
+def around(offset, n, h, w, c, dtype):
+    """Normal values about one mean, the same for every channel, so that a group's mean is `offset` of its deviations."""
+    rng = np.random.default_rng(c + h)
+    t = [offset + rng.standard_normal((n, h, w, c)), 1 + 0.2 * rng.standard_normal(c), 0.2 * rng.standard_normal(c)]
+    return [torch.from_numpy(v.astype(np.float32)).to(api.torch_dtype(dtype)) for v in t]
+
+
+# in one pass and in two, with groups of whole vectors and without, in several parts, and in column tiles that end inside a group
+FAR = [(1, 12, 12, 64, 8), (1, 70, 70, 64, 8), (2, 5, 3, 90, 9), (1, 41, 37, 90, 9), (1, 200, 190, 24, 3), (1, 50, 37, 2056, 8)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("dtype,offset", [(F32, 30.0), (F32, -300.0), (BF16, 30.0)])
+@pytest.mark.parametrize("n,h,w,c,groups", FAR)
+def test_groups_whose_mean_is_many_deviations(n, h, w, c, groups, dtype, offset, fp8):
+    check(n, h, w, c, groups, dtype, api.TT_ACT_NONE, fp8, tensors=around(offset, n, h, w, c, dtype))
+
+
+@pytest.mark.parametrize("offset", [30.0, -300.0])
+@pytest.mark.parametrize("n,h,w,c,groups", FAR[:2])
+def test_means_of_squares_in_32_bits_would_not_do(n, h, w, c, groups, offset):
+    """What the test above is there for: E[x^2] - E[x]^2 from float32 sums is outside its tolerance."""
+    x, gamma, beta = around(offset, n, h, w, c, F32)
+    y, tol = reference(x, gamma, beta, groups, api.TT_ACT_NONE, 1e-5)
+    flat = x.numpy().reshape(n, h * w, groups, c // groups).transpose(0, 2, 1, 3).reshape(n, groups, -1)
+    size = np.float32(flat.shape[2])
+    mean = np.cumsum(flat, axis=2, dtype=np.float32)[..., -1] / size
+    var = np.cumsum(flat * flat, axis=2, dtype=np.float32)[..., -1] / size - mean * mean
+    spread = lambda t: np.repeat(t, c // groups, axis=1).reshape(n, 1, 1, c).astype(np.float64)  # noqa: E731
+    with np.errstate(invalid="ignore"):
+        naive = (x.double().numpy() - spread(mean)) / np.sqrt(spread(var) + 1e-5) * gamma.double().numpy() + beta.double().numpy()
+    assert not (np.abs(naive - y) <= tol).all()
+
+
 # An activation's own error.  GELU: test_fp8.py's bound.  SiLU, v / (1 + exp(-v)): a product, a sum, an exponential and a reciprocal of
 # less than 2^-20 together, and the exponent, rounded with its constant, by 1.5 * 2^-24 of |v|; a reciprocal below 2^-126 is 0.
 @pytest.mark.gpu
