@@ -14,10 +14,11 @@
 // of a turn are taken in the next reading turn, so that no wave waits for a product's latency.
 // A step's scales, 256 of A and as many of B, come into the LDS with the operands, in a ring of four.
 //
-// 8192^3: 454 us (2.42 PFLOP/s), a scale per row of B 20 % more (eight FMAs and products an instruction for four).  The card's power
-// sets its clock: 1.98 GHz, and 2.4 on operands of zeros, 371 us in as many cycles; without the operands' requests it takes 416 us,
-// without the stores of the results 455.  Fragments read a turn ahead, and two quadrants a turn with half the barriers,
-// took the same time to a percent.
+// 8192^3: 472 us called in turn on three sets of operands (2.33 PFLOP/s), a scale per row of B 20 % more (eight FMAs and products an
+// instruction for four).  The card's power sets its clock, so that the time depends on what ran before: 448 us at best, 500 where launches
+// are traced apart, and 374 on operands of zeros, in as many cycles.  Before the scales were raised (454 us for 462 now) it took 416 us
+// without the operands' requests and 455 without the stores of the results; fragments read a turn ahead, and two quadrants a turn with
+// half the barriers, took the same time to a percent.
 #pragma once
 
 #include "fp8_product.hip.h"

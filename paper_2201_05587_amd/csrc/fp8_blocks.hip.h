@@ -72,7 +72,7 @@ __device__ __forceinline__ uint32_t largest_of_16_lanes(uint32_t v)
 }
 // x Phi(x) = max(x, 0) - |x| Q(|x|), Q(a) = 1 - Phi(a).  exp(a^2 / 2) Q(a) falls smoothly from 1/2 like 1 / (a sqrt(2 pi)) and is, to 5.5e-8
 // of itself, a polynomial of degree 8 in t = 1 / (1 + 0.3 a) (fitted to scipy's erfcx on a <= 12; beyond, exp(-a^2 / 2) ends it).  Against the
-// value in 64 bits: 2.4e-7 at most, 7.6e-7 of it down to x = -4; below, 2^-20 of it and 1.3 x^2 2^-24 (exp2's argument is rounded), some of what a
+// value in 64 bits: 2.4e-7 at most, 7.6e-7 of it down to x = -4; below, 2^-20 of it and 1.3 x^2 2^-24 (exp2's argument is rounded), about what a
 // rounding of x changes, and nothing from x = -13.2 on, where exp2 ends.  Some 20 instructions without a branch, where the compiler's erff
 // takes 60: 1024 x 768 x 768 with GELU 6.8 -> 5.5 us, 9 x 7 x 90 7.0 -> 6.2.
 __device__ __forceinline__ float gelu_smooth(float x)

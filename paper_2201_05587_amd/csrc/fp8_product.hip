@@ -12,12 +12,12 @@ namespace {
 // Estimated times (us) of a launch, fitted to launches of 1 .. 8192 rows by 64 .. 32768 columns by 64 .. 16384, 1 to 256 in a batch.
 //
 // bf16, a scale in 128 rows of B, tiles of 64 | 128 | blocks:
-//   m x 4096 x 4096, m = 256  13.3 | 24.3 | 47     512  17.5 | 24.8 | 47     1024  31 | 26.4 | 48     2048  62 | 58 | 50     4096  129 | 100 | 62
-//   4096 x 768 x 768  8.5 | 9.5 | 15.4     1024 x 768 x 768  4.8 | 8.4 | 14.7     8192^3  903 | 716 | 454     8192 x 8192 x 64  52 | 66 | 36
+//   m x 4096 x 4096, m = 256  13.2 | 24.5 | 49     512  18 | 24.9 | 49     1024  33 | 26.9 | 50     2048  57 | 51 | 52     4096  122 | 102 | 61
+//   4096 x 768 x 768  7.9 | 9.2 | 15.8     1024 x 768 x 768  4.7 | 8.5 | 15.1     8192^3  852 | 715 | 448     8192 x 8192 x 64  54 | 69 | 36
 // Rounds of workgroups over the CUs; of 64 x 64 a CU takes three together, and one alone is no faster than its loads.  Further:
-//   fp32 widens its operands, which costs the smaller tile more: m x 4096 x 4096, m = 512  29 | 35     1024  49 | 38     4096  179 | 144;
-//   a scale in every row of B is a product more for each output: 3012 x 2982 x 1601  31 | 41 | 32;
-//   rows of bf16 that start at odd elements are stored by halves, 64 KB of a block by one CU: 302 x 247 x 467  4.0 | 7.7 | 17.4.
+//   fp32 widens its operands, which costs the smaller tile more: m x 4096 x 4096, m = 512  28 | 38     1024  49 | 41     4096  176 | 152;
+//   a scale in every row of B is a product more for each output: 3012 x 2982 x 1601  31 | 43 | 34;
+//   rows of bf16 that start at odd elements are stored by halves, 64 KB of a block by one CU: 302 x 247 x 467  4.1 | 7.3 | 15.5 (248: 11.1).
 double estimate_tiles(int tile, const tt_fp8_shape &s, int64_t tiles, int64_t steps, int64_t cus)
 {
     const double full = (double)tiles / (double)cus, rounds = (double)((tiles + cus - 1) / cus), k = (double)steps;
@@ -34,8 +34,9 @@ double estimate_tiles(int tile, const tt_fp8_shape &s, int64_t tiles, int64_t st
 
 // The streaming kernel reads A again for 16 rows of B, so that it leads while its workgroups are few (us, stream | tiles, their
 // reduction split where that is faster):
-//   1 x 4096 x 4096  5.6 | 8.2     12 x 4096 x 4096  6.6 | 8.5     32 x 4096 x 4096  9.1 | 9.4     24 x 1000 x 2048 fp32  5.2 | 8.0
-//   1 x 8192 x 8192  16.0 | 14.1   32 x 8192 x 8192  28 | 15.1     1 x 32768 x 1024  15.0 | 7.4    16 batches of 32 x 512 x 512  5.5 | 3.9
+//   1 x 4096 x 4096  5.6 | 8.3     12 x 4096 x 4096  6.6 | 8.7     32 x 4096 x 4096  9.1 | 9.5     24 x 1000 x 2048 fp32  5.3 | 7.8
+//   1 x 8192 x 8192  16.1 | 14.3   32 x 8192 x 8192  28.7 | 15.3   1 x 32768 x 1024  15.6 | 7.3    16 batches of 32 x 512 x 512  5.6 | 3.9
+// The estimates count no bytes from memory: all of these found their weights in the memory-side cache.
 constexpr int kStreamRows = 32;
 double estimate_stream(int64_t rows, int64_t workgroups, int64_t steps, int64_t cus)
 {
@@ -68,7 +69,7 @@ int plan_of(const tt_fp8_shape &s, tt_fp8_launch *l)
     if (!f32) consider(estimate_tiles(256, s, tiles(256, 256) * s.batch, kb, cus), TT_FP8_BLOCKS, 256, 256, Fp8Block::THREADS, Fp8Block::LDS);
     if (s.m <= kStreamRows) consider(estimate_stream(s.m, tiles(kStreamRows, 16) * s.batch, kb, cus), TT_FP8_STREAM, s.m <= 16 ? 16 : 32, 16, 512, 0);
     // Few tiles and a long reduction: splits of it, whose sums a second launch adds, from a workspace written and read.
-    // 100 x 512 x 8192: 21 us, 4 splits 11.1, 8 10.6, 16 13.5; 300 x 1000 x 1000 7.8 us, 2 splits 8.9; 200 x 8192 x 4096 17.9 us, 8 splits 38.
+    // 100 x 512 x 8192: 21 us, 4 splits 10.9, 8 9.7, 16 11.0; 300 x 1000 x 1000 5.2 us, 2 splits 7.6; 200 x 8192 x 4096 17.5 us, 8 splits 38.
     int splits = 1;
     for (int n = 2; n <= 16 && n * 2 <= kb; n *= 2) {
         const double sums = 2.5 + 0.35 * n + (double)n * s.batch * s.m * s.n * 4 / 2.5e6;
