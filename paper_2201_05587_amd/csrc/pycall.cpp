@@ -228,7 +228,9 @@ public:
         if (!is_tensor(o)) return address_of(o);
         const at::Tensor &t = THPVariable_Unpack(o);
         good_ = good_ && t.scalar_type() == type && t.numel() == numel && t.is_contiguous() && on_device(t);
-        return good_ ? address_of(o) : nullptr;
+        void *const p = good_ ? address_of(o) : nullptr;
+        good_ = p != nullptr; // (a tensor without memory is not an argument left out)
+        return p;
     }
     // A workspace is memory of any type; `bytes`: how many there are.
     void *workspace(PyObject *o, size_t *bytes)

@@ -562,6 +562,29 @@ def test_tensors_of_other_classes_on_the_gpu():
     assert status(lambda: api.tt_dense_fp8(*a, *w, None, api.tt_fp8_shape(1, 100, 512, 8192, 128, BF16), api.TT_DENSE_ADD, ws=ws)) == api.TT_ERR_BAD_ARG
 
 
+class WithoutMemory(torch.Tensor):
+    """A tensor that says what it is and holds nothing, as wrappers of other tensors do: its address is 0."""
+
+    @staticmethod
+    def __new__(cls, *sizes):
+        return torch.Tensor._make_wrapper_subclass(cls, sizes, dtype=torch.float32, device=f"cuda:{torch.cuda.current_device()}")
+
+    @classmethod
+    def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+        raise RuntimeError("holds nothing")
+
+
+@pytest.mark.gpu
+def test_a_tensor_without_memory_is_no_argument_left_out():
+    x = api.tt_quantize_fp8(torch.randn(8, 200, device="cuda"), api.tt_quant_shape(1, 8, 200, 1, F32))
+    shape = api.tt_fp8_shape(1, 8, 8, 200, 1, F32)
+    assert status(lambda: api.tt_dense_fp8(*x, *x, WithoutMemory(8), shape, api.TT_DENSE_ADD)) == api.TT_ERR_BAD_ARG
+    v, norm = torch.randn(1, 2, 2, 8, device="cuda"), api.tt_norm_shape(1, 2, 2, 8, 2, F32)
+    for weights in ((WithoutMemory(8), None), (None, WithoutMemory(8))):
+        assert status(lambda: api.tt_group_norm_act(v, *weights, norm)) == api.TT_ERR_BAD_ARG
+    assert status(lambda: api.tt_group_norm_act(WithoutMemory(1, 2, 2, 8), None, None, norm)) == api.TT_ERR_BAD_ARG
+
+
 @pytest.mark.gpu
 def test_the_binding_refuses_other_types_sizes_and_strides_on_the_gpu():
     bad = api.TT_ERR_BAD_ARG
